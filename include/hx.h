@@ -24,6 +24,7 @@
 #ifndef HX_H_
 #define HX_H_
 
+#include <stddef.h>
 #include <stdint.h>
 
 #ifdef __cplusplus
@@ -540,6 +541,154 @@ int hx_decode_set_running(hx_cluster* h, const uint32_t* inst_ptr, const hx_kv_i
 int hx_schedule_decode(hx_cluster* h, const hx_call* calls, const int32_t* lock, const float* ready_s,
                        int n_calls, int32_t* out_inst, float* out_start, float* out_ratio,
                        int32_t* out_order, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * Paged KV cache of a decode (or prefill) instance, and the attention that
+ * reads it.  The planners count KV tokens (Eq. 3, 4); here are the pages that
+ * hold them: sibling calls of a workflow share the pages of their common
+ * prompt, finished calls give theirs back, prompts arrive from the prefill
+ * side, and the free tokens go back into the scheduler's table.
+ *
+ * hx_kv_cache describes a cache (host struct, read during the call); every
+ * pointer in it is a device buffer of the caller on the handle's device.
+ *   k, v: keys and values, element (layer, page, token, head, i) at
+ *     layer * layer_stride + page * page_stride + (token * n_kv_heads + head)
+ *     * head_dim + i.  Strides in elements; strides and the bytes of a token are
+ *     multiples of 16 bytes, the base addresses 16-byte aligned.
+ *   table[max_seqs][max_pages]: the pages of every sequence in order, -1 behind
+ *     its last one.  len[max_seqs]: its tokens.  A sequence of length 0 is an
+ *     empty slot.
+ *   ref[n_pages]: how many entries of the table name the page; 0 = free.  A
+ *     caller may hold pages of its own by a larger count.
+ *   work: int32[HX_KV_WORK(n_pages, max_seqs)], scratch of the calls on this
+ *     cache.  Two calls on one cache, or on descriptions that share `work`,
+ *     must not overlap on the GPU: keep them on one stream, replayed graphs too.
+ * A page that is not full belongs to one sequence alone (fork copies it), so
+ * what is written behind a sequence's end is seen by no other.
+ *   New pages are the lowest-numbered ones free at the start of the call, in
+ * the order of the requests; request i is granted when it takes none or when
+ * all requests up to i together need no more than were free.  A request that is
+ * not granted leaves its sequence as it was and gets out_ok 0 (out_ok: device
+ * int32[n] or NULL); one with an id out of range, a sequence named a second
+ * time, a broken length or page entry likewise, and raises HX_ERR_INVALID_ARG in
+ * the status word.  Pages given back by a call are free after it.
+ *   out: where the changed tables go, NULL = in place; else three other arrays of
+ * the same sizes, written whole, while the cache's own stay as they are.  (Data
+ * is moved in the pools either way, into pages that were free.)
+ *   All calls only enqueue on `stream`, allocate nothing, and may be captured.
+ * n <= max_seqs requests. */
+#define HX_DTYPE_F16  0
+#define HX_DTYPE_BF16 1
+#define HX_DTYPE_F32  2     /* page operations only */
+#define HX_DTYPE_U8   3     /* page operations only: any 8-bit type */
+
+#define HX_KV_MAX_SEQS   16384
+#define HX_KV_MAX_PAGES  1048576
+#define HX_KV_MAX_LAYERS 1024
+#define HX_KV_WORK(n_pages, max_seqs) ((size_t)(n_pages) + 5 * (size_t)(max_seqs) + 8)
+
+typedef struct { int32_t *ref, *table, *len; } hx_kv_tables;
+
+typedef struct {
+    int32_t n_pages, page_tokens, max_seqs, max_pages;
+    int32_t n_layers, n_kv_heads, head_dim, dtype;
+    int64_t layer_stride, page_stride;
+    void *k, *v;
+    int32_t *ref, *table, *len, *work;
+} hx_kv_cache;
+
+/* Checks a description without touching a device; the message is hx_last_error(NULL). */
+int hx_kv_check(const hx_kv_cache* cache);
+
+/* dst[i] becomes a copy of the first keep[i] tokens of src[i] (keep NULL = all of
+ * them; the parent's state at the start of the call): whole pages are shared,
+ * the used rows of a partly used last one are copied to a new page.  What dst[i]
+ * held is given back.  src[i] == dst[i] cuts a sequence short.  No other
+ * request may rewrite a sequence that a request reads (refused like a bad id). */
+int hx_kv_fork(hx_cluster* h, const hx_kv_cache* cache, const int32_t* src, const int32_t* dst,
+               const int32_t* keep, int n, const hx_kv_tables* out, int32_t* out_ok, void* stream);
+
+/* Gives the pages of n sequences back and empties their slots. */
+int hx_kv_free(hx_cluster* h, const hx_kv_cache* cache, const int32_t* seqs, int n,
+               const hx_kv_tables* out, void* stream);
+
+/* Makes n sequences counts[i] tokens longer (room for rows that hx_kv_write fills). */
+int hx_kv_grow(hx_cluster* h, const hx_kv_cache* cache, const int32_t* seqs, const int32_t* counts,
+               int n, const hx_kv_tables* out, int32_t* out_ok, void* stream);
+
+/* Writes the last cu[i + 1] - cu[i] tokens of sequence seqs[i] in one layer, for
+ * sequences that have been grown already.  cu: device int32[n + 1], cu[0] = 0.  Token t
+ * (0 <= t < n_rows, n_rows >= cu[n]) takes row rows[t] of k_new / v_new (device
+ * int32[n_rows]; NULL: row t), each row n_kv_heads * head_dim elements at
+ * row * row_stride, n_src rows; so the accepted ones of drafted tokens can be
+ * picked out.  Requests with ok[i] == 0 are skipped (ok NULL: none). */
+int hx_kv_write(hx_cluster* h, const hx_kv_cache* cache, int layer, const int32_t* seqs, const int32_t* cu,
+                int n, const void* k_new, const void* v_new, int64_t row_stride, int n_rows,
+                const int32_t* rows, int n_src, const int32_t* ok, void* stream);
+
+/* Copies sequences src[i] of `from` into slots dst[i] of `cache`, whose pages may have
+ * another size (the KV transfer of a placement, Section 4.2); what dst[i] held is given
+ * back.  The caches agree in layers, heads, head_dim and element type and are not the same. */
+int hx_kv_copy(hx_cluster* h, const hx_kv_cache* from, const hx_kv_cache* cache, const int32_t* src,
+               const int32_t* dst, int n, const hx_kv_tables* out, int32_t* out_ok, void* stream);
+
+/* Packs the pool: with U pages in use, those numbered U and above move, in order, to the
+ * free numbers below U, and every table entry follows.  out_goes: device int32[n_pages], the
+ * new number of every page in use, -1 for the others. */
+int hx_kv_compact(hx_cluster* h, const hx_kv_cache* cache, const hx_kv_tables* out, int32_t* out_goes,
+                  void* stream);
+
+/* Free pages x page_tokens become the free KV tokens of decode instance d in the cluster's
+ * table, where the capacity pass and the greedy planner read them: on the device, without a
+ * copy to the host.  Needs a pool of less than 2^24 tokens. */
+int hx_kv_report(hx_cluster* h, const hx_kv_cache* cache, int decode_instance, void* stream);
+
+/* Attention over a paged cache (F16 or BF16; head_dim 64, 96 or 128; n_q_heads a multiple of
+ * n_kv_heads, query head h reads KV head h / (n_q_heads / n_kv_heads)):
+ *   out = sum_j softmax_j(scale * q . k_j) v_j,  lse = log sum_j exp(scale * q . k_j)
+ * over the rows j that a query sees.  Sums, maxima and the result are held in binary32; the weights
+ * are rounded to the element type for the product with the values.  A query that sees
+ * nothing gets zeros and lse -inf; rows that a query does not see have no part in its result whatever they hold
+ * (infinities and NaN too).
+ *   q, out: element (row, head, i) at row * row_stride + head * head_stride + i; q 16-byte
+ * aligned with strides that are multiples of 8 elements, out 4-byte aligned with even strides.  lse:
+ * binary32 [n_rows][n_q_heads] or NULL.  work: hx_attend_work bytes, 16-byte aligned, free to use again when the
+ * call's work is done; calls that may overlap on the GPU need one each.
+ *   seqs: device int32[n], the cache's sequences.  A sequence with an id or length out of range raises
+ * HX_ERR_INVALID_ARG in the status word and its rows are left as they were; an entry of its table that names no page
+ * raises it too and is not seen. */
+typedef struct {
+    const void* q; int64_t q_row_stride, q_head_stride;
+    void* out; int64_t out_row_stride, out_head_stride;
+    float* lse;
+    void* work; size_t work_bytes;
+    int32_t n_rows, n_q_heads;
+    float scale;
+} hx_attend_io;
+
+/* Bytes of scratch that an attention call on this cache needs at most, for any batch.  Returns HX_OK or
+ * HX_ERR_INVALID_ARG (message: hx_last_error(NULL)); touches no device. */
+int hx_attend_work(const hx_kv_cache* cache, int n_q_heads, size_t* bytes);
+
+/* Sliding window with sinks, for prefill, chunks of it, and decode (one query a call).  The queries of sequence i are rows
+ * cu[i] .. cu[i + 1] - 1 (device int32[n + 1], ascending, at most max_q each) and stand at the last
+ * positions of the sequence, whose keys and values are in the cache already (hx_kv_write).  The query at
+ * position p sees position j <= p when j > p - window (the window counts p itself) or j < sinks.  Rows of
+ * q behind cu[n] are not touched. */
+int hx_attend_window(hx_cluster* h, const hx_kv_cache* cache, int layer, const hx_attend_io* io, const int32_t* seqs,
+                     const int32_t* cu, int n, int max_q, int window, int sinks, void* stream);
+
+/* A tree of drafted tokens behind each sequence: rows i * n_draft + t of q, k_draft and v_draft (element (row, head, e) of
+ * the latter at row * draft_row_stride + head * head_dim + e; 16-byte aligned, stride a multiple of 8) are the n_draft <=
+ * HX_TREE_MAX drafted tokens of sequence i.  parents: device int32[n][n_draft], the row of a token's parent (lower than its
+ * own), -1 = its parent is the sequence's last token, -2 = there is no such token (a tree smaller than
+ * the widest: zeros and lse -inf).  A drafted token sees the whole sequence, its ancestors and itself; one below a token
+ * that is not there, or with another parent number, counts as -2 (the latter raises HX_ERR_INVALID_ARG in the status
+ * word).  The drafted rows are not in the cache; write the accepted ones with hx_kv_grow and hx_kv_write. */
+#define HX_TREE_MAX 128
+int hx_attend_tree(hx_cluster* h, const hx_kv_cache* cache, int layer, const hx_attend_io* io, const void* k_draft,
+                   const void* v_draft, int64_t draft_row_stride, const int32_t* parents, const int32_t* seqs, int n,
+                   int n_draft, void* stream);
 
 /* Borrowed device pointers to the top-K results of the last batch scored with
  * topk = K > 0: pairs int32[n_calls][K] (-1 = unused slot), costs

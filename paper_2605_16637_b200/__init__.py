@@ -13,7 +13,10 @@ from .api import (CALL_DTYPE, INSTANCE_DTYPE, HX_FLAG_NO_DAG, HX_FLAG_NO_TAIL, H
                   hx_dag_append, hx_earliest_start, hx_get_earliest_results,
                   hx_get_status, hx_get_topk, hx_last_error, hx_launch_count, hx_schedule_batch,
                   hx_schedule_batch_host, hx_schedule_batch_host_async, hx_schedule_sweep_host, hx_set_attention_flops, hx_schedule_batch_static, hx_schedule_greedy, hx_schedule_greedy_plan, hx_replay, hx_replay_lifecycle, hx_measure_fp32_rates, hx_dag_append_workflows, hx_estimate_calls,
-                  hx_decode_set_running, hx_schedule_decode, KV_INTERVAL_DTYPE, hx_set_options, lib_path)
+                  hx_decode_set_running, hx_schedule_decode, KV_INTERVAL_DTYPE, hx_set_options, lib_path,
+                  HX_DTYPE_F16, HX_DTYPE_BF16, HX_DTYPE_F32, HX_DTYPE_U8, HX_KV_MAX_SEQS, HX_KV_MAX_PAGES, HX_KV_MAX_LAYERS,
+                  HX_KV_WORK, HX_TREE_MAX, KvCache, hx_kv_check, hx_kv_fork, hx_kv_free, hx_kv_grow, hx_kv_write, hx_kv_copy,
+                  hx_kv_compact, hx_kv_report, hx_attend_work, hx_attend_window, hx_attend_tree)
 
 __all__ = [n for n in dir() if n.startswith(("hx_", "HX_", "Hx")) or n in
-           ("CALL_DTYPE", "INSTANCE_DTYPE", "KV_INTERVAL_DTYPE", "Cluster", "lib_path")]
+           ("CALL_DTYPE", "INSTANCE_DTYPE", "KV_INTERVAL_DTYPE", "KvCache", "Cluster", "lib_path")]

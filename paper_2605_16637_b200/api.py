@@ -30,6 +30,33 @@ class HxError(RuntimeError):
         self.code = code
 
 
+HX_DTYPE_F16, HX_DTYPE_BF16, HX_DTYPE_F32, HX_DTYPE_U8 = 0, 1, 2, 3
+HX_KV_MAX_SEQS, HX_KV_MAX_PAGES, HX_KV_MAX_LAYERS, HX_TREE_MAX = 16384, 1048576, 1024, 128
+
+
+def HX_KV_WORK(n_pages, max_seqs):
+    """int32 words of scratch that a cache needs."""
+    return n_pages + 5 * max_seqs + 8
+
+
+class _KvTables(C.Structure):
+    _fields_ = [("ref", C.c_void_p), ("table", C.c_void_p), ("len", C.c_void_p)]
+
+
+class _KvCache(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_pages", "page_tokens", "max_seqs", "max_pages", "n_layers", "n_kv_heads",
+                                         "head_dim", "dtype")] + \
+               [("layer_stride", C.c_int64), ("page_stride", C.c_int64)] + \
+               [(n, C.c_void_p) for n in ("k", "v", "ref", "table", "len", "work")]
+
+
+class _AttendIo(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("q_row_stride", C.c_int64), ("q_head_stride", C.c_int64),
+                ("out", C.c_void_p), ("out_row_stride", C.c_int64), ("out_head_stride", C.c_int64),
+                ("lse", C.c_void_p), ("work", C.c_void_p), ("work_bytes", C.c_size_t),
+                ("n_rows", C.c_int32), ("n_q_heads", C.c_int32), ("scale", C.c_float)]
+
+
 class _Options(C.Structure):
     _fields_ = [("score_mode", C.c_int), ("topk", C.c_int), ("commit", C.c_int),
                 ("flags", C.c_int), ("alpha", C.c_float)]
@@ -74,6 +101,17 @@ def _load():
         "hx_estimate_calls": [vp, vp, ci, vp, vp, vp, vp, vp],
         "hx_decode_set_running": [vp, vp, vp, vp],
         "hx_schedule_decode": [vp, vp, vp, vp, ci, vp, vp, vp, vp, vp],
+        "hx_kv_check": [C.POINTER(_KvCache)],
+        "hx_kv_fork": [vp, C.POINTER(_KvCache), vp, vp, vp, ci, C.POINTER(_KvTables), vp, vp],
+        "hx_kv_free": [vp, C.POINTER(_KvCache), vp, ci, C.POINTER(_KvTables), vp],
+        "hx_kv_grow": [vp, C.POINTER(_KvCache), vp, vp, ci, C.POINTER(_KvTables), vp, vp],
+        "hx_kv_write": [vp, C.POINTER(_KvCache), ci, vp, vp, ci, vp, vp, C.c_int64, ci, vp, ci, vp, vp],
+        "hx_kv_copy": [vp, C.POINTER(_KvCache), C.POINTER(_KvCache), vp, vp, ci, C.POINTER(_KvTables), vp, vp],
+        "hx_kv_compact": [vp, C.POINTER(_KvCache), C.POINTER(_KvTables), vp, vp],
+        "hx_kv_report": [vp, C.POINTER(_KvCache), ci, vp],
+        "hx_attend_work": [C.POINTER(_KvCache), ci, C.POINTER(C.c_size_t)],
+        "hx_attend_window": [vp, C.POINTER(_KvCache), ci, C.POINTER(_AttendIo), vp, vp, ci, ci, ci, ci, vp],
+        "hx_attend_tree": [vp, C.POINTER(_KvCache), ci, C.POINTER(_AttendIo), vp, vp, C.c_int64, vp, vp, ci, ci, vp],
         "hx_get_topk": [vp, C.POINTER(vp), C.POINTER(vp), C.POINTER(vp)],
         "hx_get_status": [vp, C.POINTER(ci), vp],
         "hx_measure_fp32_rates": [vp, vp, vp, vp],
@@ -325,6 +363,59 @@ def hx_schedule_sweep_host(h, calls, chunk_calls, kv_free_reset, out_assign, out
                                        _p(out_assign), _p(out_cost), stream), h)
 
 
+def hx_kv_check(cache):
+    """Checks the description of a cache (the `c` of a KvCache, or None) without touching a device."""
+    _check(_lib.hx_kv_check(cache), None)
+
+
+def hx_kv_fork(h, cache, src_ptr, dst_ptr, keep_ptr, n, out=None, ok_ptr=None, stream=0):
+    """dst becomes a copy of (the first keep tokens of) src; device pointers, out a _KvTables or None (in place)."""
+    _check(_lib.hx_kv_fork(h, cache, src_ptr, dst_ptr, keep_ptr, int(n), out, ok_ptr, stream), h)
+
+
+def hx_kv_free(h, cache, seqs_ptr, n, out=None, stream=0):
+    _check(_lib.hx_kv_free(h, cache, seqs_ptr, int(n), out, stream), h)
+
+
+def hx_kv_grow(h, cache, seqs_ptr, counts_ptr, n, out=None, ok_ptr=None, stream=0):
+    _check(_lib.hx_kv_grow(h, cache, seqs_ptr, counts_ptr, int(n), out, ok_ptr, stream), h)
+
+
+def hx_kv_write(h, cache, layer, seqs_ptr, cu_ptr, n, k_ptr, v_ptr, row_stride, n_rows, rows_ptr, n_src, ok_ptr=None,
+                stream=0):
+    _check(_lib.hx_kv_write(h, cache, int(layer), seqs_ptr, cu_ptr, int(n), k_ptr, v_ptr, int(row_stride), int(n_rows),
+                            rows_ptr, int(n_src), ok_ptr, stream), h)
+
+
+def hx_kv_copy(h, source, cache, src_ptr, dst_ptr, n, out=None, ok_ptr=None, stream=0):
+    _check(_lib.hx_kv_copy(h, source, cache, src_ptr, dst_ptr, int(n), out, ok_ptr, stream), h)
+
+
+def hx_kv_compact(h, cache, out, goes_ptr, stream=0):
+    _check(_lib.hx_kv_compact(h, cache, out, goes_ptr, stream), h)
+
+
+def hx_kv_report(h, cache, decode_instance, stream=0):
+    _check(_lib.hx_kv_report(h, cache, int(decode_instance), stream), h)
+
+
+def hx_attend_work(cache, n_q_heads):
+    """Bytes of scratch of an attention call; touches no device."""
+    need = C.c_size_t(0)
+    _check(_lib.hx_attend_work(cache, int(n_q_heads), C.byref(need)), None)
+    return need.value
+
+
+def hx_attend_window(h, cache, layer, io, seqs_ptr, cu_ptr, n, max_q, window, sinks, stream=0):
+    _check(_lib.hx_attend_window(h, cache, int(layer), io, seqs_ptr, cu_ptr, int(n), int(max_q), int(window), int(sinks),
+                                 stream), h)
+
+
+def hx_attend_tree(h, cache, layer, io, k_ptr, v_ptr, draft_row_stride, parents_ptr, seqs_ptr, n, n_draft, stream=0):
+    _check(_lib.hx_attend_tree(h, cache, int(layer), io, k_ptr, v_ptr, int(draft_row_stride), parents_ptr, seqs_ptr,
+                               int(n), int(n_draft), stream), h)
+
+
 def hx_get_topk(h):
     """Device addresses (int) of pairs, costs, prio."""
     a, b, c = C.c_void_p(), C.c_void_p(), C.c_void_p()
@@ -383,12 +474,70 @@ def _dev_to_numpy(ptr, count, typestr):
     return torch.as_tensor(_Borrowed(ptr, count, typestr), device="cuda").cpu().numpy()
 
 
+def _ints(t, name, device, shape=None):
+    """The address of an int32 tensor, or None; refuses what the C side would read wrongly."""
+    import torch
+    if t is None:
+        return None
+    if t.dtype != torch.int32 or not t.is_contiguous() or t.device != device:
+        raise HxError(-1, "%s must be a contiguous int32 tensor on %s" % (name, device))
+    if shape is not None and tuple(t.shape) != shape:
+        raise HxError(-1, "%s must have shape %s, not %s" % (name, shape, tuple(t.shape)))
+    return t.data_ptr()
+
+
+class KvCache:
+    """A paged KV cache over the caller's tensors: keys and values [layers, pages, page tokens, KV heads, head_dim] (layers and
+    pages may be strided), reference counts [pages], page table [sequences, columns] and lengths [sequences] (int32).
+    Keeps the tensors alive, and the scratch of the calls on it: use one cache on one stream at a time."""
+
+    def __init__(self, k, v, ref, table, length, work=None):
+        import torch
+        kinds = {torch.float16: HX_DTYPE_F16, torch.bfloat16: HX_DTYPE_BF16, torch.float32: HX_DTYPE_F32}
+        if k.dim() != 5 or k.shape != v.shape or k.dtype != v.dtype or k.stride() != v.stride() or k.device != v.device:
+            raise HxError(-1, "keys and values must agree: [layers, pages, page tokens, heads, head_dim], one type, one layout")
+        layers, pages, tokens, heads, dim = k.shape
+        if k.numel() and k.stride()[2:] != (heads * dim, dim, 1):
+            raise HxError(-1, "the tokens of a page must be contiguous")
+        if k.dtype not in kinds and k.element_size() != 1:
+            raise HxError(-1, "a cache holds float16, bfloat16, float32 or an 8-bit type")
+        if table.dim() != 2:
+            raise HxError(-1, "the table must be [sequences, columns]")
+        if work is None:
+            work = torch.empty(HX_KV_WORK(pages, table.shape[0]), dtype=torch.int32, device=k.device)
+        elif work.numel() < HX_KV_WORK(pages, table.shape[0]):
+            raise HxError(-1, "work is smaller than HX_KV_WORK says")
+        self.device, self.k, self.v, self.ref, self.table, self.length, self.work = k.device, k, v, ref, table, length, work
+        self.layers, self.n_pages, self.page_tokens, self.heads, self.dim = layers, pages, tokens, heads, dim
+        self.max_seqs, self.max_pages = table.shape
+        self.c = _KvCache(pages, tokens, self.max_seqs, self.max_pages, layers, heads, dim,
+                          kinds.get(k.dtype, HX_DTYPE_U8), k.stride(0) if layers > 1 else tokens * heads * dim,
+                          k.stride(1) if pages > 1 else tokens * heads * dim, k.data_ptr(), v.data_ptr(),
+                          _ints(ref, "ref", k.device, (pages,)), _ints(table, "table", k.device),
+                          _ints(length, "length", k.device, (self.max_seqs,)), _ints(work, "work", k.device))
+        hx_kv_check(self.c)
+        self.tables = _KvTables(self.c.ref, self.c.table, self.c.len)
+        self._scratch = {}
+
+    def with_tables(self, ref, table, length):
+        """The same pool under other tables (what a call wrote elsewhere)."""
+        return KvCache(self.k, self.v, ref, table, length, self.work)
+
+    def attend_bytes(self, q_heads):
+        """Scratch of an attention call (hx_attend_work), asked once."""
+        if q_heads not in self._scratch:
+            self._scratch[q_heads] = hx_attend_work(self.c, q_heads)
+        return self._scratch[q_heads]
+
+
 class Cluster:
     """Owns one hx_cluster handle; methods mirror the C entry points."""
 
     def __init__(self, gpu_types, instances, link_bw_gbps, models):
         self.h = None
         self.h = hx_cluster_create(gpu_types, instances, link_bw_gbps, models)
+        import torch
+        self.device = torch.device("cuda", torch.cuda.current_device())      # where the handle's tables are
         inst = _np(instances, INSTANCE_DTYPE)
         self.P = int((inst["role"] == 0).sum())
         self.D = int(inst.shape[0] - self.P)
@@ -549,6 +698,127 @@ class Cluster:
                            ratio.data_ptr(), order.data_ptr(), self._stream())
         torch.cuda.current_stream().synchronize()      # lk / rd are temporaries of this call
         return inst, start, ratio, order
+
+    # --- paged KV cache and the attention that reads it (device tensors; int32 ids and counts) -------------------
+
+    def _on(self, cache, out=None):
+        """The stream to enqueue on; refuses a cache of another device and tables of another shape."""
+        import torch
+        if cache.device != self.device:
+            raise HxError(-1, "the cache is on %s, the cluster on %s" % (cache.device, self.device))
+        if out is not None and (out.n_pages, out.max_seqs, out.max_pages) != (cache.n_pages, cache.max_seqs, cache.max_pages):
+            raise HxError(-1, "the new tables have other sizes than the cache's")
+        return torch.cuda.current_stream(self.device).cuda_stream
+
+    def _ok(self, n):
+        import torch
+        return torch.empty(n, dtype=torch.int32, device=self.device)
+
+    def kv_fork(self, cache, src, dst, keep=None, out=None):
+        """dst[i] becomes a copy of the first keep[i] (all) tokens of src[i]; returns 1 for each request granted.  out: a
+        KvCache whose tables are written instead of the cache's own."""
+        n, dev = src.numel(), self.device
+        stream, ok = self._on(cache, out), self._ok(n)
+        hx_kv_fork(self.h, cache.c, _ints(src, "src", dev), _ints(dst, "dst", dev, (n,)), _ints(keep, "keep", dev, (n,)), n,
+                   None if out is None else out.tables, ok.data_ptr(), stream)
+        return ok
+
+    def kv_free(self, cache, seqs, out=None):
+        hx_kv_free(self.h, cache.c, _ints(seqs, "seqs", self.device), seqs.numel(), None if out is None else out.tables,
+                   self._on(cache, out))
+
+    def kv_grow(self, cache, seqs, counts, out=None):
+        """Makes sequences counts[i] tokens longer; returns 1 for each request granted."""
+        n, dev = seqs.numel(), self.device
+        stream, ok = self._on(cache, out), self._ok(n)
+        hx_kv_grow(self.h, cache.c, _ints(seqs, "seqs", dev), _ints(counts, "counts", dev, (n,)), n,
+                   None if out is None else out.tables, ok.data_ptr(), stream)
+        return ok
+
+    def kv_write(self, cache, layer, seqs, cu, k, v, rows=None, ok=None):
+        """Writes the last cu[i + 1] - cu[i] tokens of sequence seqs[i] in one layer: row t, or row rows[t], of k and v
+        [rows, heads, head_dim] for token t."""
+        n, dev = seqs.numel(), self.device
+        for t in (k, v):
+            if t.dtype != cache.k.dtype or t.device != dev or t.dim() != 3 or t.shape[1:] != cache.k.shape[3:] or \
+                    t.shape[0] != k.shape[0] or (t.shape[0] and (t.stride()[1:] != (cache.dim, 1) or t.stride(0) != k.stride(0))):
+                raise HxError(-1, "new rows must be [rows, heads, head_dim] of the cache's type, on its device, each row contiguous")
+        stride = k.stride(0) if k.shape[0] > 1 else cache.heads * cache.dim
+        hx_kv_write(self.h, cache.c, layer, _ints(seqs, "seqs", dev), _ints(cu, "cu", dev, (n + 1,)), n, k.data_ptr(), v.data_ptr(),
+                    stride, k.shape[0] if rows is None else rows.numel(), _ints(rows, "rows", dev), k.shape[0],
+                    _ints(ok, "ok", dev, (n,)), self._on(cache))
+
+    def kv_copy(self, source, cache, src, dst, out=None):
+        """Copies sequences src[i] of another cache into slots dst[i]; returns 1 for each request granted."""
+        n, dev = src.numel(), self.device
+        self._on(source)
+        stream, ok = self._on(cache, out), self._ok(n)
+        hx_kv_copy(self.h, source.c, cache.c, _ints(src, "src", dev), _ints(dst, "dst", dev, (n,)), n,
+                   None if out is None else out.tables, ok.data_ptr(), stream)
+        return ok
+
+    def kv_compact(self, cache, out=None):
+        """Packs the pool to its low end; returns the new number of every page in use (-1: free)."""
+        stream, goes = self._on(cache, out), self._ok(cache.n_pages)
+        hx_kv_compact(self.h, cache.c, None if out is None else out.tables, goes.data_ptr(), stream)
+        return goes
+
+    def kv_report(self, cache, decode_instance):
+        """The pool's free tokens become the free KV tokens of a decode instance in the scheduler's table."""
+        hx_kv_report(self.h, cache.c, decode_instance, self._on(cache))
+
+    def _attend_io(self, cache, q, scale, out, lse):
+        """(description, out, lse, scratch) of an attention call over rows q [rows, heads, head_dim]."""
+        import torch
+        dev = self.device
+        if q.dim() != 3 or q.shape[2] != cache.dim or q.dtype != cache.k.dtype or q.device != dev or (q.numel() and q.stride(2) != 1):
+            raise HxError(-1, "q must be [rows, heads, head_dim] of the cache's type, on its device, heads contiguous")
+        rows, heads = q.shape[:2]
+        if out is None:
+            out = torch.empty(q.shape, dtype=q.dtype, device=dev)
+        elif out.shape != q.shape or out.dtype != q.dtype or out.device != dev or (out.numel() and out.stride(2) != 1):
+            raise HxError(-1, "out must be like q")
+        if lse is None:
+            lse = torch.empty((rows, heads), dtype=torch.float32, device=dev)
+        elif lse.shape != (rows, heads) or lse.dtype != torch.float32 or lse.device != dev or not lse.is_contiguous():
+            raise HxError(-1, "lse must be a contiguous float32 tensor [rows, heads]")
+        need = cache.attend_bytes(heads)
+        work = torch.empty(need, dtype=torch.uint8, device=dev)
+        # the stride of a dimension of one element is never used and may be anything
+        strides = [t.stride(i) if t.shape[i] > 1 else cache.dim for t in (q, out) for i in (0, 1)]
+        io = _AttendIo(q.data_ptr(), strides[0], strides[1], out.data_ptr(), strides[2], strides[3], lse.data_ptr(), work.data_ptr(), need, rows, heads, cache.dim ** -0.5 if scale is None else scale)
+        return io, out, lse, work
+
+    def attend_window(self, cache, layer, q, seqs, cu, max_q, window, sinks=0, scale=None, out=None, lse=None):
+        """Attention of the last cu[i + 1] - cu[i] <= max_q tokens of sequences seqs[i] (rows of q) with a sliding window
+        and first tokens that stay visible.  Returns (out, lse)."""
+        n, dev, stream = seqs.numel(), self.device, self._on(cache)
+        io, out, lse, work = self._attend_io(cache, q, scale, out, lse)
+        if q.shape[0] == 0:
+            return out, lse
+        hx_attend_window(self.h, cache.c, layer, io, _ints(seqs, "seqs", dev), _ints(cu, "cu", dev, (n + 1,)), n, max_q, window,
+                         sinks, stream)
+        return out, lse
+
+    def attend_tree(self, cache, layer, q, k_draft, v_draft, seqs, parents, scale=None, out=None, lse=None):
+        """Attention of drafted tokens (rows i * n_draft + t of q, k_draft, v_draft) over sequences seqs[i] and their own
+        ancestors; parents [n, n_draft].  Returns (out, lse)."""
+        n, dev, stream = seqs.numel(), self.device, self._on(cache)
+        if parents.dim() != 2 or parents.shape[0] != n:
+            raise HxError(-1, "parents must be [sequences, drafted tokens]")
+        for t in (k_draft, v_draft):
+            if t.dtype != cache.k.dtype or t.device != dev or t.shape != (q.shape[0], cache.heads, cache.dim) or \
+                    (t.numel() and (t.stride()[1:] != (cache.dim, 1) or t.stride(0) != k_draft.stride(0))):
+                raise HxError(-1, "drafted rows must be [rows of q, KV heads, head_dim] of the cache's type, each row contiguous")
+        if q.shape[0] != parents.numel():
+            raise HxError(-1, "q must have one row per drafted token")
+        io, out, lse, work = self._attend_io(cache, q, scale, out, lse)
+        if q.shape[0] == 0:
+            return out, lse
+        stride = k_draft.stride(0) if k_draft.shape[0] > 1 else cache.heads * cache.dim
+        hx_attend_tree(self.h, cache.c, layer, io, k_draft.data_ptr(), v_draft.data_ptr(), stride, _ints(parents, "parents", dev),
+                       _ints(seqs, "seqs", dev), n, parents.shape[1], stream)
+        return out, lse
 
     def schedule_batch_host(self, calls, out_assign=None, out_cost=None):
         return hx_schedule_batch_host(self.h, calls, out_assign, out_cost, self._stream())

@@ -505,6 +505,7 @@ void hx_cluster_shape(const hx_cluster* h, int* P, int* D, const float** capD_de
     *n_nodes = h->dag_uploaded ? h->N : 0; *n_workflows = h->dag_uploaded ? h->W : 0;
 }
 hx_options hx_current_options(const hx_cluster* h) { return h->opts; }
+HxCore hx_core(hx_cluster* h) { return HxCore{h->device, h->n_sm, h->D, h->status, &h->launches, h->tab.freeD}; }
 
 int hx_update_loads_packed(hx_cluster* h, const float* packed, cudaStream_t s) {
     const size_t n = (size_t)h->P + 2 * (size_t)h->D;

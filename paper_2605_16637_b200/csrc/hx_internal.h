@@ -214,6 +214,10 @@ cudaError_t hx_launch_cost_update(const HxForestDev& f, const uint32_t* idx, con
 int hx_fail(hx_cluster* h, int code, const char* msg);            // records msg as the last error, returns code
 void hx_cluster_shape(const hx_cluster* h, int* P, int* D, const float** capD_dev, uint32_t* n_nodes, uint32_t* n_workflows);
 hx_options hx_current_options(const hx_cluster* h);
+// What the entry points of other files need of a handle.
+struct HxCore { int device, n_sm, D; int* status; long long* launches; float* freeD; };
+HxCore hx_core(hx_cluster* h);
+const char* hx_kv_why_not(const hx_kv_cache* c);                  // why a cache description is refused, NULL = it is fine
 // Classes of the instances (prefill first, then decode) and the reciprocal link table, read back from the device.
 int hx_cluster_tables_host(hx_cluster* h, std::vector<int>* typeP, std::vector<int>* typeD, std::vector<float>* invLT,
                            int* Ppad, int* G, int* M, cudaStream_t s);

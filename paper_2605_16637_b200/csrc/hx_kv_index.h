@@ -1,0 +1,74 @@
+// Index arithmetic of the paged KV cache and of the attention that reads it, as plain functions of whole numbers:
+// the kernels call them, and they compile with an ordinary C++ compiler too, so that every bound can be checked
+// without a GPU.
+#ifndef HX_KV_INDEX_H_
+#define HX_KV_INDEX_H_
+
+#include <stdint.h>
+
+#ifdef __CUDACC__
+#define HX_HD __host__ __device__ __forceinline__
+#else
+#define HX_HD inline
+#endif
+
+// Page that holds position pos of a sequence, or -1 when the position lies behind the row of the table or the entry
+// names no page of the pool: such a position is never read or written.
+HX_HD int hx_page_at(const int32_t* row, int max_pages, int n_pages, int page_tokens, int pos) {
+    const int c = pos / page_tokens;
+    if (pos < 0 || c >= max_pages) return -1;
+    const int p = row[c];
+    return (p >= 0 && p < n_pages) ? p : -1;
+}
+
+HX_HD int hx_ceil_div(int a, int b) { return a / b + (a % b != 0); }
+
+// Length of a sequence as the kernels take it: what the table row can hold at most, and no less than nothing.
+HX_HD int hx_len_ok(int len, int max_pages, int page_tokens) {
+    return len >= 0 && (int64_t)len <= (int64_t)max_pages * page_tokens;
+}
+
+// The positions that at least one query of a tile sees, as one axis without the gap between the first tokens and the
+// window: entry x is position x below n_sink and x + gap from there on; n entries.
+struct HxAxis { int n_sink, gap, n; };
+
+// Queries at positions p_first .. p_last, each of which sees j <= p with j > p - window or j < sinks.
+HX_HD HxAxis hx_window_axis(int p_first, int p_last, int window, int sinks) {
+    const int hi = p_last + 1;
+    int lo = p_first - window + 1;                       // p_first >= 0, window >= 0: no overflow
+    if (lo < 0) lo = 0;
+    int n_sink = sinks < lo ? sinks : lo;
+    if (n_sink > hi) n_sink = hi;
+    HxAxis a;
+    a.n_sink = n_sink;
+    a.gap = lo - n_sink;
+    a.n = n_sink + (hi > lo ? hi - lo : 0);
+    return a;
+}
+HX_HD int hx_axis_pos(const HxAxis& a, int x) { return x < a.n_sink ? x : x + a.gap; }
+
+HX_HD bool hx_window_sees(int p, int j, int window, int sinks) { return j <= p && (j > p - window || j < sinks); }
+
+// Whether every query of p_first .. p_last sees every entry of [xa, xb] (xb < a.n): no mask is needed there.
+HX_HD bool hx_window_full(const HxAxis& a, int xa, int xb, int p_first, int p_last, int window, int sinks) {
+    if (xb >= a.n || hx_axis_pos(a, xb) > p_first) return false;
+    int x = xa > a.n_sink ? xa : a.n_sink;
+    int px = x + a.gap;
+    if (px < sinks) px = sinks;
+    return px > p_last - window;
+}
+
+// Tiles of the axis, at least one so that rows that see nothing are written too.
+HX_HD int hx_tiles(int n, int tile) { return n > tile ? hx_ceil_div(n, tile) : 1; }
+
+// Share c of n_shares of `total` units: [hx_share(c), hx_share(c + 1)).
+HX_HD int64_t hx_share(int64_t total, int c, int n_shares) { return total * c / n_shares; }
+// The share that holds unit u: the largest c with hx_share(total, c, n) <= u (0 <= u < total).
+HX_HD int hx_share_of(int64_t total, int64_t u, int n_shares) {
+    int c = (int)((u * n_shares) / total);
+    while (c + 1 < n_shares && hx_share(total, c + 1, n_shares) <= u) ++c;
+    while (c > 0 && hx_share(total, c, n_shares) > u) --c;
+    return c;
+}
+
+#endif  // HX_KV_INDEX_H_
