@@ -1,16 +1,31 @@
 // Attention over a paged KV cache: a sliding window with first tokens that stay visible, and trees of drafted tokens.
 //
-// Work is a list of groups: the queries of one sequence that share a KV head, M rows at a time (row r is query r / G,
-// head r % G of the G query heads), against the tokens that any of them sees.  The tokens form one axis without gaps
-// (first tokens, then window; or cached tokens, then drafted ones) cut into tiles of 64.
+// Work is a list of groups: up to 256 rows of the queries of one sequence that share a KV head (row r is query r / G, head
+// r % G of the G query heads), against the tokens that any of them sees.  The tokens form one axis without gaps (first tokens,
+// then window; or cached tokens, then drafted ones), cut into tiles of 128.
 //
-// Few groups: the tiles of all groups form one line that is cut into equal shares, one per block, so that ragged
-// lengths cost nothing; a group that is cut leaves partial results (maximum, sum, weighted values) that a
-// second launch joins in a fixed order.  Many groups: a block takes whole groups in turn.
+// Few groups: the tiles of all groups form one line that is cut into equal shares, one per multiprocessor, so that ragged
+// lengths cost nothing; a group that is cut leaves partial results (maximum, sum, weighted values) that a second launch
+// joins in a fixed order.  Many groups: a block takes whole groups in turn.
 //
-// A tile goes to shared memory with 16-byte asynchronous copies, addressed row by row through the page table (any page
-// size), two tiles ahead of the products; the table is read one tile ahead of that.  Products are mma.sync m16n8k16 with
-// binary32 sums; weights stay in registers.
+// One block per multiprocessor, four warpgroups:
+//   0, 1  softmax of two streams: a thread holds one row of scores (128 tokens) in registers
+//   2     one warp loads: rows of tokens by TMA, four at a time by their row numbers (gather), which each lane takes
+//         from the page table, so any page size will do; a ring of keys and values runs ahead across groups; three warps
+//         load the rows of q
+//   3     one warp issues the tensor-core products (tcgen05, 128 x 128 tiles), one looks the next groups up
+// Scores S = Q K^T go to tensor memory, the weights P return there in the cache's type as the left operand of O += P V, and
+// O stays there in binary32 for the whole group.  A group of more than 128 rows gives each stream 128 of them against
+// the same tiles; a smaller one gives the streams alternate tiles of the same rows, joined at its end.  So one stream's
+// products run while the other's exponentials do.
+//
+// The maximum that the weights are taken against follows the true one only when that has grown by more than 2^8: O is
+// rescaled then.  Weights are at most 2^8 that way, the sums are in binary32, and the result does not depend on the choice but for rounding.
+//
+// A value that some queries of a tile do not see may be infinite or NaN, and 0 x NaN is NaN in the product.  The tiles that need
+// masks (the ends of a group) are therefore looked through; where one holds such a value the block says so, and the second launch
+// computes that block's groups again with one warp per row, which reads only what the row sees.
+#include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -22,17 +37,23 @@
 
 namespace {
 
-constexpr int BN = 64;               // tokens per tile
-constexpr int THREADS = 128;
-constexpr int STAGES = 3;
-constexpr int SLOTS = STAGES + 2;    // rings of row addresses run this far ahead
-constexpr int PLAN_ITEMS = 1024;     // row tiles that the shared plan holds
+constexpr int BN = 128;              // tokens per tile
+constexpr int TILE_ROWS = 128;       // rows of one stream's product
+constexpr int GROUP_ROWS = 256;
+constexpr int THREADS = 512;
+constexpr int PLAN_ITEMS = 1024;     // groups per head that the shared plan holds
+constexpr int GROUP_COST = 1;        // tiles that the start and end of a group are worth
+constexpr int SEGS = 2;              // groups looked up ahead
+constexpr int VALID_RING = 8;
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+constexpr float GROWTH = 8.f;        // powers of two that the maximum may grow before O is rescaled
+constexpr unsigned long long WAIT_NS = 2000000000ull;    // a wait that lasts this long ends the kernel with HX_ERR_TIMEOUT
 
 struct AttendArgs {
     // cache
     const char *k, *v;               // of the layer
-    int64_t page_bytes;
+    int page_rows;                   // tokens from one page to the next in memory
+    int chunk;                       // tokens that are loaded together: a power of two that divides a page, 1 = gathered by four
     int token_bytes, page_tokens, n_pages, max_seqs, max_pages, n_kv_heads;
     const int32_t *table, *len;
     // rows
@@ -43,74 +64,127 @@ struct AttendArgs {
     float scale_log2;
     // requests
     const int32_t *seqs, *cu, *parents;
-    int n, max_q, row_tiles;         // row tiles of a sequence: ceil(max_q * G / M)
+    int n, max_q, row_tiles;         // groups of a sequence and head: ceil(max_q * G / 256)
     int window, sinks;
     const char *k_draft, *v_draft; int64_t draft_row_bytes;
-    int tree, planned;               // planned: shares of the line of tiles; else whole groups in turn
+    int tree, planned, out16;        // planned: shares of the line of tiles; else whole groups in turn; out16: 16-byte stores
     // partial results
     float* part; int4* desc;
     int* status;
 };
 
-// One group: what the loader and the products need of it.
+// One group: what the loads and the products need of it.
 struct Group {
     int item, head, tiles;
     int seq, row0, nq, len;          // slot of the cache, first row of q, queries, tokens
-    int r0;                          // first of its rows
-    HxAxis axis;                     // tree: n_sink = cached tokens, n = those and the drafted ones
+    int r0, rows;                    // its first row, its rows (at most 256)
+    HxAxis axis;                     // tree: n_sink = cached tokens up to a multiple of the chunk, n = those and the drafted ones
 };
 
 template <class T> struct Elem;
 template <> struct Elem<__half> {
-    static constexpr uint32_t EXP = 0x7c00;
+    static constexpr uint32_t EXP = 0x7c00, FORMAT = 0;
     static __device__ __forceinline__ uint32_t pack(float a, float b) { __half2 h = __floats2half2_rn(a, b); return *reinterpret_cast<uint32_t*>(&h); }
-    static __device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-    }
-    static constexpr uint32_t ONE = 0x3c00;
+    static __device__ __forceinline__ float2 unpack(uint32_t x) { return __half22float2(*reinterpret_cast<__half2*>(&x)); }
 };
 template <> struct Elem<__nv_bfloat16> {
-    static constexpr uint32_t EXP = 0x7f80;
+    static constexpr uint32_t EXP = 0x7f80, FORMAT = 1;
     static __device__ __forceinline__ uint32_t pack(float a, float b) { __nv_bfloat162 h = __floats2bfloat162_rn(a, b); return *reinterpret_cast<uint32_t*>(&h); }
-    static __device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-    }
-    static constexpr uint32_t ONE = 0x3f80;
+    static __device__ __forceinline__ float2 unpack(uint32_t x) { return __bfloat1622float2(*reinterpret_cast<__nv_bfloat162*>(&x)); }
 };
 
+// ---- instructions -----------------------------------------------------------------------------------------------
+
 __device__ __forceinline__ uint32_t smem_at(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
-// 16 bytes to shared memory, zeros when src is NULL.
-__device__ __forceinline__ void copy16(uint32_t dst, const char* src, const char* any) {
-    const int bytes = src ? 16 : 0;
-    asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16, %2;" :: "r"(dst), "l"(src ? src : any), "r"(bytes) : "memory");
+__device__ __forceinline__ void copy16(uint32_t dst, const char* src, int bytes) {
+    asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16, %2;" :: "r"(dst), "l"(src), "r"(bytes) : "memory");
 }
-__device__ __forceinline__ void ldsm4(uint32_t (&r)[4], uint32_t a) {
-    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(a) : "memory");
-}
-__device__ __forceinline__ void ldsm4t(uint32_t (&r)[4], uint32_t a) {
-    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(a) : "memory");
-}
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 __device__ __forceinline__ float exp2_fast(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
 
-// Packed pairs of elements that are infinite or NaN, and which.
-template <class T> __device__ __forceinline__ bool odd_pair(uint32_t x) {
-    return (x & Elem<T>::EXP) == Elem<T>::EXP || (x & (Elem<T>::EXP << 16)) == (Elem<T>::EXP << 16);
+__device__ __forceinline__ void bar_init(uint32_t bar, int count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" :: "r"(bar), "r"(count) : "memory"); }
+__device__ __forceinline__ void bar_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" :: "r"(bar) : "memory"); }
+__device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.b32 %0, 1, 0, p;\n}" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+    return ok != 0;
 }
-// The element at `sh` split: finite part, and a one in plus / minus / nan when it is infinite or NaN.
-template <class T> __device__ __forceinline__ void split_pair(uint32_t x, uint32_t& fin, uint32_t& plus, uint32_t& minus, uint32_t& nan) {
-    fin = x; plus = minus = nan = 0;
-#pragma unroll
-    for (int sh = 0; sh < 32; sh += 16) {
-        const uint32_t e = (x >> sh) & 0xffffu;
-        if ((e & Elem<T>::EXP) != Elem<T>::EXP) continue;
-        fin &= ~(0xffffu << sh);
-        const uint32_t one = Elem<T>::ONE << sh;
-        if (e & 0x7fffu & ~Elem<T>::EXP) nan |= one;
-        else if (e & 0x8000u) minus |= one;
-        else plus |= one;
+__device__ __forceinline__ unsigned long long now_ns() { unsigned long long t; asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t)); return t; }
+// False when the block is to end: this wait or another has lasted too long.
+__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile int* quit) {
+    if (bar_try(bar, parity)) return true;
+    const unsigned long long t0 = now_ns();
+    for (uint32_t i = 1;; ++i) {
+        if (bar_try(bar, parity)) return true;
+        if ((i & 63) == 0) {
+            if (*quit) return false;
+            if (now_ns() - t0 > WAIT_NS) { *quit = 1; return false; }
+        }
     }
+}
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int* quit) {
+    return __all_sync(0xffffffffu, bar_wait(bar, parity, quit));
+}
+__device__ __forceinline__ bool elect() {
+    uint32_t one;
+    asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.b32 %0, 1, 0, p;\n}" : "=r"(one));
+    return one != 0;
+}
+__device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes) {
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" :: "r"(bar), "r"(bytes) : "memory");
+}
+// Four rows of 64 elements, by number, from column x of the map; rows behind its end come as zeros.
+__device__ __forceinline__ void gather4(uint32_t dst, const CUtensorMap* map, int x, int4 rows, uint32_t bar) {
+    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile::gather4.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];"
+                 :: "r"(dst), "l"(map), "r"(x), "r"(rows.x), "r"(rows.y), "r"(rows.z), "r"(rows.w), "r"(bar) : "memory");
+}
+// Rows y .. of the map's box, 64 elements from column x each.
+__device__ __forceinline__ void load_box(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
+    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+                 :: "r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
+__device__ __forceinline__ void tc_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_commit(uint32_t bar) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" :: "r"(bar) : "memory");
+}
+__device__ __forceinline__ void tc_mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t add) {
+    asm volatile("{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}"
+                 :: "r"(d), "l"(a), "l"(b), "r"(idesc), "r"(add) : "memory");
+}
+__device__ __forceinline__ void tc_mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t add) {
+    asm volatile("{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}"
+                 :: "r"(d), "r"(a), "l"(b), "r"(idesc), "r"(add) : "memory");
+}
+__device__ __forceinline__ void tc_ld32(uint32_t* r, uint32_t at) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31]) : "r"(at) : "memory");
+}
+__device__ __forceinline__ void tc_st8(uint32_t at, const uint32_t* r) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                 :: "r"(at), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]) : "memory");
+}
+__device__ __forceinline__ void tc_ld16(uint32_t* r, uint32_t at) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]) : "r"(at) : "memory");
+}
+__device__ __forceinline__ void tc_st16(uint32_t at, const uint32_t* r) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+                 :: "r"(at), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
+}
+__device__ __forceinline__ void tc_ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tc_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// Shared-memory matrix of 128-byte rows, swizzled in blocks of eight rows (1024 bytes); `lead`: bytes from one 64-element
+// panel to the next where the panels run along the operand's contiguous side (values), unused otherwise.
+__device__ __forceinline__ uint64_t matrix(uint32_t at, uint32_t lead) {
+    return (uint64_t)((at & 0x3ffff) >> 4) | (uint64_t)((lead & 0x3ffff) >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 | 1ull << 46 | 2ull << 61;
+}
+// binary32 sums, both operands of type FORMAT, 128 rows, n columns; the right operand with its n side contiguous or its k side.
+__host__ __device__ constexpr uint32_t product(uint32_t format, int n, bool n_contiguous) {
+    return 1u << 4 | format << 7 | format << 10 | (n_contiguous ? 1u << 16 : 0u) | (uint32_t)(n >> 3) << 17 | (uint32_t)(TILE_ROWS >> 4) << 24;
 }
 
 // ---- groups ---------------------------------------------------------------------------------------------------
@@ -129,573 +203,801 @@ __device__ __forceinline__ bool request(const AttendArgs& a, int b, int* seq, in
     return ok;
 }
 
-template <int M>
-__device__ __forceinline__ HxAxis group_axis(const AttendArgs& a, int nq, int len, int r0) {
-    if (a.tree) { HxAxis x; x.n_sink = len; x.gap = 0; x.n = len + nq; return x; }
-    const int last = min(nq * a.group, r0 + M) - 1;
-    return hx_window_axis(len - nq + r0 / a.group, len - nq + last / a.group, a.window, a.sinks);
-}
-
-// Tiles of row tile `item`, 0 when it has no rows.
-template <int M>
-__device__ __forceinline__ int item_tiles(const AttendArgs& a, int item, bool report) {
-    int seq, row0, nq, len;
-    const int b = item / a.row_tiles, r0 = (item - b * a.row_tiles) * M;
-    const bool ok = request(a, b, &seq, &row0, &nq, &len);
-    if (!ok) { if (report && r0 == 0) atomicExch(a.status, HX_ERR_INVALID_ARG); return 0; }
-    if (r0 >= nq * a.group) return 0;
-    return hx_tiles(group_axis<M>(a, nq, len, r0).n, BN);
-}
-
-template <int M>
 __device__ __forceinline__ Group group_of(const AttendArgs& a, int item, int head, bool report = false) {
     Group g;
-    g.item = item; g.head = head;
+    g.item = item; g.head = head; g.tiles = 0;
     const int b = item / a.row_tiles;
-    g.r0 = (item - b * a.row_tiles) * M;
+    g.r0 = (item - b * a.row_tiles) * GROUP_ROWS;
     if (!request(a, b, &g.seq, &g.row0, &g.nq, &g.len) && report && g.r0 == 0 && head == 0) atomicExch(a.status, HX_ERR_INVALID_ARG);
-    if (g.r0 >= g.nq * a.group) { g.tiles = 0; return g; }
-    g.axis = group_axis<M>(a, g.nq, g.len, g.r0);
+    g.rows = min(GROUP_ROWS, g.nq * a.group - g.r0);
+    g.axis.n_sink = g.axis.gap = g.axis.n = 0;
+    if (g.rows <= 0) { g.rows = 0; return g; }
+    if (a.tree) { g.axis.n_sink = hx_round_up(g.len, max(a.chunk, 4)); g.axis.n = g.axis.n_sink + g.nq; }
+    else g.axis = hx_window_axis(g.len - g.nq + g.r0 / a.group, g.len - g.nq + (g.r0 + g.rows - 1) / a.group, a.window, a.sinks, a.chunk);
     g.tiles = hx_tiles(g.axis.n, BN);
     return g;
 }
 
-// Where a walk over units stands.
-struct Cursor {
+// The line of tiles: prefix[i] = units before item i, per head (a group counts its tiles and GROUP_COST).
+struct Plan { int64_t total; int shares; };
+__device__ Plan make_plan(const AttendArgs& a, int64_t* prefix, int64_t* scan, int n_blocks, bool report) {
+    const int tid = threadIdx.x, nt = blockDim.x, lane = tid & 31, warp = tid >> 5, items = a.n * a.row_tiles;
+    const int per = hx_ceil_div(items, nt), i0 = min(items, tid * per), i1 = min(items, i0 + per);
+    int64_t sum = 0;
+    for (int i = i0; i < i1; ++i) {
+        const int t = group_of(a, i, 0, report).tiles, u = t ? t + GROUP_COST : 0;
+        prefix[i] = u; sum += u;
+    }
+    int64_t incl = sum;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) { const int64_t t = __shfl_up_sync(0xffffffffu, incl, o); if (lane >= o) incl += t; }
+    if (lane == 31) scan[warp] = incl;
+    __syncthreads();
+    int64_t before = incl - sum, all = 0;
+    for (int w = 0; w < nt / 32; ++w) { if (w < warp) before += scan[w]; all += scan[w]; }
+    for (int i = i0; i < i1; ++i) { const int64_t u = prefix[i]; prefix[i] = before; before += u; }
+    if (tid == 0) prefix[items] = all;
+    __syncthreads();
+    Plan p;
+    p.total = all * a.n_kv_heads;
+    // a share holds at least one tile of every group that begins before it and ends behind it
+    p.shares = (int)min((int64_t)n_blocks, max((int64_t)1, p.total / (GROUP_COST + 1)));
+    return p;
+}
+
+// A walk over the groups of block `block`.
+struct Walk {
+    int64_t unit, end, step;
+};
+__device__ __forceinline__ Walk begin_walk(const AttendArgs& a, const Plan& p, int block, int n_blocks) {
+    Walk w;
+    if (a.planned) {
+        w.unit = block < p.shares ? hx_share(p.total, block, p.shares) : 0;
+        w.end = block < p.shares ? hx_share(p.total, block + 1, p.shares) : 0;
+        w.step = 0;
+    } else {
+        w.unit = block; w.end = (int64_t)a.n * a.row_tiles * a.n_kv_heads; w.step = n_blocks;
+    }
+    return w;
+}
+// The next group that has tiles here: tiles [*t0, *t1) of it.  False at the end.  *start: unit of its first tile.
+__device__ __forceinline__ bool next_group(const AttendArgs& a, const int64_t* prefix, Walk& w, Group* g, int* t0, int* t1, int64_t* start) {
+    const int items = a.n * a.row_tiles;
+    while (w.unit < w.end) {
+        if (!a.planned) {
+            *g = group_of(a, (int)(w.unit / a.n_kv_heads), (int)(w.unit % a.n_kv_heads), true);
+            w.unit += w.step;
+            *t0 = 0; *t1 = g->tiles; *start = 0;
+            if (g->tiles) return true;
+            continue;
+        }
+        const int64_t u = w.unit;
+        int lo = 0, hi = items;      // last item whose units begin at or before u (items without any are passed over)
+        while (hi - lo > 1) { const int m = (lo + hi) >> 1; if (prefix[m] * a.n_kv_heads <= u) lo = m; else hi = m; }
+        const int64_t units = prefix[lo + 1] - prefix[lo], in = u - prefix[lo] * a.n_kv_heads;
+        const int head = (int)(in / units);
+        const int64_t x = in - head * units, left = min(units - x, w.end - u);
+        w.unit = u + left;
+        *t0 = (int)max((int64_t)0, x - GROUP_COST);
+        *t1 = (int)max((int64_t)0, x + left - GROUP_COST);
+        if (*t1 <= *t0) continue;
+        *g = group_of(a, lo, head);
+        *t1 = min(*t1, g->tiles);    // the lengths may not change while the call runs; never behind the group all the same
+        *start = u - x + GROUP_COST;
+        if (*t1 > *t0) return true;
+    }
+    return false;
+}
+
+// A group as the roles of the block see it.
+struct Seg {
     Group g;
-    int tile;                        // in the group
-    int64_t unit, end;               // planned: unit of the line; else group number
+    int t0, t1;                      // its tiles here; t1 = t0: no more groups
+    uint4 anc[HX_TREE_MAX];          // tree: the ancestors of every drafted token, as bits; none for one that is not there
 };
 
-// Finds the group of unit u of the line: prefix[i] = tiles before item i (per head).
-template <int M>
-__device__ __forceinline__ void seek(const AttendArgs& a, const int* prefix, int items, Cursor& c) {
-    int lo = 0, hi = items;          // last item whose tiles begin at or before u (items without tiles are passed over)
-    const int64_t u = c.unit;
-    while (hi - lo > 1) { const int m = (lo + hi) >> 1; if ((int64_t)prefix[m] * a.n_kv_heads <= u) lo = m; else hi = m; }
-    const int tiles = prefix[lo + 1] - prefix[lo];
-    const int64_t in = u - (int64_t)prefix[lo] * a.n_kv_heads;
-    const int head = (int)(in / tiles);
-    c.g = group_of<M>(a, lo, head);
-    c.tile = (int)(in - (int64_t)head * tiles);
+// Ancestors of the drafted tokens of sequence b, by one warp: each round doubles how far up the bits reach.
+__device__ void ancestors(const AttendArgs& a, int b, uint4* anc, int* link) {
+    const int lane = threadIdx.x & 31, t = a.max_q;
+    uint32_t bits[4][4];
+    int up[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int i = lane + 32 * j;
+        up[j] = -2;
+        if (i < t) {
+            const int p = a.parents[(int64_t)b * t + i];
+            if (p < -2 || p >= i) atomicExch(a.status, HX_ERR_INVALID_ARG);
+            up[j] = (p < -2 || p >= i) ? -2 : p;
+            link[i] = up[j];
+        }
+#pragma unroll
+        for (int w = 0; w < 4; ++w) bits[j][w] = (i >> 5) == w ? 1u << (i & 31) : 0u;
+        if (i < t) anc[i] = make_uint4(bits[j][0], bits[j][1], bits[j][2], bits[j][3]);
+    }
+    __syncwarp();
+    for (int reach = 1; reach < t; reach *= 2) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (up[j] >= 0) {
+                const uint4 m = anc[up[j]];
+                bits[j][0] |= m.x; bits[j][1] |= m.y; bits[j][2] |= m.z; bits[j][3] |= m.w;
+                up[j] = link[up[j]];
+            }
+        __syncwarp();
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int i = lane + 32 * j;
+            if (i < t) { anc[i] = make_uint4(bits[j][0], bits[j][1], bits[j][2], bits[j][3]); link[i] = up[j]; }
+        }
+        __syncwarp();
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int i = lane + 32 * j;
+        if (i < t && up[j] != -1) anc[i] = make_uint4(0, 0, 0, 0);
+    }
 }
 
-template <int M>
-__device__ __forceinline__ void open_group(const AttendArgs& a, Cursor& c, int64_t step) {     // whole groups: the next one that has rows
-    for (; c.unit < c.end; c.unit += step) {
-        c.g = group_of<M>(a, (int)(c.unit / a.n_kv_heads), (int)(c.unit % a.n_kv_heads), true);
-        if (c.g.tiles) break;
-    }
-    c.tile = 0;
-}
-
-template <int M>
-__device__ __forceinline__ void advance(const AttendArgs& a, const int* prefix, int items, Cursor& c, int64_t step) {
-    if (a.planned) {
-        ++c.unit;
-        if (c.unit >= c.end) return;
-        if (++c.tile < c.g.tiles) return;
-        seek<M>(a, prefix, items, c);
-    } else {
-        if (++c.tile < c.g.tiles) return;
-        c.unit += step;
-        open_group<M>(a, c, step);
-    }
-}
-
-// Address of the K and V rows of entry x of the group's axis; 0 where there is none.
-__device__ __forceinline__ void row_address(const AttendArgs& a, const Group& g, int x, int row_bytes, const char** k, const char** v, bool* bad) {
-    *k = *v = nullptr;
-    if (x >= g.axis.n) return;
-    if (a.tree && x >= g.axis.n_sink) {
-        const int64_t at = (int64_t)(g.row0 + x - g.axis.n_sink) * a.draft_row_bytes + (int64_t)g.head * row_bytes;
-        *k = a.k_draft + at; *v = a.v_draft + at;
-        return;
-    }
+// Row of memory, counted in tokens, that holds entry x of the group's axis, of the cache or (*drafted) of the drafted rows; -1
+// where there is none.
+__device__ __forceinline__ int row_of(const AttendArgs& a, const Group& g, int x, bool* drafted) {
+    *drafted = a.tree && x >= g.axis.n_sink;
+    if (x >= g.axis.n) return -1;
+    if (*drafted) return g.row0 + x - g.axis.n_sink;
+    if (a.tree && x >= g.len) return -1;
     const int pos = a.tree ? x : hx_axis_pos(g.axis, x);
     const int page = hx_page_at(a.table + (int64_t)g.seq * a.max_pages, a.max_pages, a.n_pages, a.page_tokens, pos);
-    if (page < 0) { *bad = true; return; }
-    const int64_t at = page * a.page_bytes + (int64_t)(pos % a.page_tokens) * a.token_bytes + (int64_t)g.head * row_bytes;
-    *k = a.k + at; *v = a.v + at;
+    if (page < 0) { atomicExch(a.status, HX_ERR_INVALID_ARG); return -1; }
+    return page * a.page_rows + pos % a.page_tokens;
+}
+
+// Entries of [0, 32) below n, as bits.
+__device__ __forceinline__ uint32_t below(int n) { return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u; }
+
+// What row r of the group sees of entries xa .. xa + 127, as bits (entries behind the axis are the caller's to take out).
+__device__ __forceinline__ void sees(const AttendArgs& a, const Group& g, const uint4* anc, int r, int xa, uint32_t (&m)[4]) {
+    const int qi = (g.r0 + r) / a.group;
+    if (a.tree) {
+        const uint4 t = anc[qi];
+        const bool there = (t.x | t.y | t.z | t.w) != 0;
+        const uint32_t w[5] = {t.x, t.y, t.z, t.w, 0u};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int s = xa + 32 * i - g.axis.n_sink;           // drafted token of the word's first bit
+            uint32_t x = 0;
+            if (s <= -32) x = 0xffffffffu;
+            else if (s < 0) x = below(-s) | w[0] << -s;
+            else if (s < 128) {
+#pragma unroll
+                for (int k = 0; k < 4; ++k) if ((s >> 5) == k) x = __funnelshift_r(w[k], w[k + 1], s & 31);
+            }
+            m[i] = there ? x : 0u;
+        }
+        return;
+    }
+    const int p = g.len - g.nq + qi, gap = g.axis.gap;
+    int first = min(a.sinks, p + 1);                     // first tokens: entries below this
+    if (gap) first = min(first, g.axis.n_sink);
+    first -= xa;
+    const int lo = max(p - a.window + 1 - gap, g.axis.n_sink) - xa, hi = p + 1 - gap - xa;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) m[i] = below(first - 32 * i) | (below(hi - 32 * i) & ~below(lo - 32 * i));
 }
 
 template <int D> struct Shape {
     static constexpr int CHUNKS = D / 8;                       // 16-byte pieces of a row
-    static constexpr int PITCH = (CHUNKS + 7) / 8 * 8;         // padded so that the swizzle stays inside the row
-    static constexpr int TILE = BN * PITCH * 16;               // bytes of K, or V, of a tile
-    static constexpr int OPITCH = D + 8;                       // floats to a row of the joining buffer
+    static constexpr int PANELS = (D + 63) / 64;               // of 128 bytes
+    static constexpr int TILE = PANELS * 128 * 128;            // bytes of K, or V, of a tile, and of 128 rows of Q
+    static constexpr int SLOTS = PANELS == 1 ? 8 : 4;          // 128 KB of keys and values in flight
+    static constexpr int SMEM = 2 * TILE + SLOTS * TILE + 1024;
 };
-template <int D>
-__device__ __forceinline__ uint32_t piece(int row, int c) { return (uint32_t)(row * Shape<D>::PITCH + (c ^ (row & 7))) * 16; }
+// Byte of piece c of row r of a tile.
+__device__ __forceinline__ uint32_t piece(int r, int c) { return (uint32_t)((c >> 3) * 16384 + r * 128 + (((c & 7) ^ (r & 7)) << 4)); }
 
-template <int D>
-constexpr size_t smem_bytes() {
-    return (size_t)STAGES * 2 * Shape<D>::TILE + SLOTS * BN * 16 + SLOTS * 4 + (PLAN_ITEMS + 1) * 4 + HX_TREE_MAX * 20 + 16;
-}
+struct Shared {
+    Seg seg[SEGS];
+    int64_t prefix[PLAN_ITEMS + 1];
+    int64_t scan[THREADS / 32];
+    alignas(16) uint32_t valid[VALID_RING][4];   // entries of a tile that have a row
+    float2 stat[TILE_ROWS];          // maximum and sum of the second stream, where it shares its rows
+    int link[HX_TREE_MAX];
+    int4 rows[4][32];                // row numbers of the tiles being loaded, four to a lane; -1: zeros
+    unsigned long long full[8], empty[8], q_full, q_empty, s_full[2], p_full[2], o_full[2], x_ready, x_free, seg_full[SEGS], seg_empty[SEGS], drained;
+    uint32_t tmem;
+    int quit;
+};
 
-// WM warps along the rows (16 each), 4 / WM along the tokens of a tile.
-template <int D, int WM, class T>
-__global__ void __launch_bounds__(THREADS, 2) hx_attend_kernel(const AttendArgs a) {
-    constexpr int M = 16 * WM, WN = 4 / WM, NW = BN / WN, NT = NW / 8, KT = NW / 16, DT = D / 8, KD = D / 16;
-    constexpr int ROW_BYTES = D * 2;
-    extern __shared__ __align__(128) char smem[];
-    char* tiles_s = smem;
-    const char** addr = reinterpret_cast<const char**>(smem + STAGES * 2 * Shape<D>::TILE);      // [SLOTS][2][BN]
-    int* broken = reinterpret_cast<int*>(addr + SLOTS * 2 * BN);                                 // [SLOTS]
-    int* prefix = broken + SLOTS;                                                                // [PLAN_ITEMS + 1]
-    uint4* anc = reinterpret_cast<uint4*>((reinterpret_cast<uintptr_t>(prefix + PLAN_ITEMS + 1) + 15) & ~(uintptr_t)15);   // [HX_TREE_MAX]
-    int* par = reinterpret_cast<int*>(anc + HX_TREE_MAX);                                        // [HX_TREE_MAX]
-    __shared__ int scan[8];
+// Places of tile j's keys and values in the order in which a group of n tiles is loaded.
+__device__ __forceinline__ int key_place(bool pair, int n, int j) { return pair ? 2 * j : j == 0 ? 0 : 2 * j - 1; }
+__device__ __forceinline__ int value_place(bool pair, int n, int j) { return pair ? 2 * j + 1 : j + 1 < n ? 2 * j + 2 : 2 * n - 1; }
 
+struct Maps { CUtensorMap k, v, k_draft, v_draft; };     // rows of tokens: of the cache's layer, and drafted ones
+
+template <int D, class T>
+__global__ void __launch_bounds__(THREADS, 1) hx_attend_kernel(const AttendArgs a, const __grid_constant__ Maps maps) {
+    using S = Shape<D>;
+    constexpr int NS = S::SLOTS;
+    extern __shared__ char smem_raw[];
+    char* smem = reinterpret_cast<char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+    char *q_s = smem, *kv_s = smem + 2 * S::TILE;
+    __shared__ Shared sh;
+    volatile int* quit = &sh.quit;
+
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, role = warp >> 2;
+    if (warp == 0) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" :: "r"(smem_at(&sh.tmem)) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    if (tid == 32) {
+        for (int i = 0; i < NS; ++i) { bar_init(smem_at(&sh.full[i]), 1); bar_init(smem_at(&sh.empty[i]), 1); }
+        bar_init(smem_at(&sh.q_full), 96); bar_init(smem_at(&sh.q_empty), 1);
+        for (int i = 0; i < 2; ++i) { bar_init(smem_at(&sh.s_full[i]), 1); bar_init(smem_at(&sh.p_full[i]), 4); bar_init(smem_at(&sh.o_full[i]), 1); }
+        bar_init(smem_at(&sh.x_ready), 4); bar_init(smem_at(&sh.x_free), 4);
+        for (int i = 0; i < SEGS; ++i) { bar_init(smem_at(&sh.seg_full[i]), 1); bar_init(smem_at(&sh.seg_empty[i]), 13); }
+        bar_init(smem_at(&sh.drained), 1);
+        sh.quit = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
     hx_wait_for_primary();
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int wm = warp / WN, wn = warp % WN, lg = lane >> 2, lq = lane & 3;
-    const int items = a.n * a.row_tiles;
-
-    // ---- what this block does
-    Cursor ld, cs;
-    int64_t step = gridDim.x, total = 0;
-    int shares = 1;
-    if (a.planned) {
-        const int per = hx_ceil_div(items, THREADS), i0 = min(items, tid * per), i1 = min(items, i0 + per);
-        int sum = 0;
-        for (int i = i0; i < i1; ++i) { const int t = item_tiles<M>(a, i, blockIdx.x == 0); prefix[i] = t; sum += t; }
-        int incl = sum;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) { const int t = __shfl_up_sync(0xffffffffu, incl, o); if (lane >= o) incl += t; }
-        if (lane == 31) scan[warp] = incl;
-        __syncthreads();
-        int before = incl - sum, all = 0;
-        for (int w = 0; w < 4; ++w) { if (w < warp) before += scan[w]; all += scan[w]; }
-        for (int i = i0; i < i1; ++i) { const int t = prefix[i]; prefix[i] = before; before += t; }
-        if (tid == 0) prefix[items] = all;
-        __syncthreads();
-        total = (int64_t)all * a.n_kv_heads;
-        if (tid == 0) a.desc[blockIdx.x] = make_int4(0, 0, 0, 0);
-        shares = (int)min((int64_t)gridDim.x, total);    // so that no share is empty
-        if ((int)blockIdx.x >= shares) return;
-        ld.unit = hx_share(total, blockIdx.x, shares);
-        ld.end = hx_share(total, blockIdx.x + 1, shares);
-        seek<M>(a, prefix, items, ld);
-    } else {
-        ld.unit = blockIdx.x;
-        ld.end = (int64_t)items * a.n_kv_heads;
-        open_group<M>(a, ld, step);
-        if (ld.unit >= ld.end) return;
-    }
-    cs = ld;
-    const int64_t first_unit = ld.unit;
-    Cursor lk = ld;                                      // looks addresses up, ahead of the loader
-
-    auto look_up = [&](const char** k, const char** v, bool* bad) {     // threads 0 .. BN - 1
-        *bad = false;
-        *k = *v = nullptr;
-        if (lk.unit < lk.end && tid < BN) row_address(a, lk.g, lk.tile * BN + tid, ROW_BYTES, k, v, bad);
-    };
-    auto put_address = [&](int tile_no, const char* k, const char* v, bool bad) {
-        if (tid < BN) {
-            const int slot = tile_no % SLOTS;
-            addr[(slot * 2) * BN + tid] = k; addr[(slot * 2 + 1) * BN + tid] = v;
-            if (bad) { broken[slot] = tile_no; atomicExch(a.status, HX_ERR_INVALID_ARG); }
-        }
-    };
-    auto load_tile = [&](int stage, int slot) {
-        constexpr int C = Shape<D>::CHUNKS;
-        const uint32_t base = smem_at(tiles_s + stage * 2 * Shape<D>::TILE);
-#pragma unroll
-        for (int kv = 0; kv < 2; ++kv)
-#pragma unroll
-            for (int j = 0; j < BN * C / THREADS; ++j) {
-                const int e = j * THREADS + tid, row = e / C, c = e - row * C;
-                const char* src = addr[(slot * 2 + kv) * BN + row];
-                copy16(base + kv * Shape<D>::TILE + piece<D>(row, c), src ? src + c * 16 : nullptr, a.k);
-            }
-    };
-    auto fence_group = [] { asm volatile("cp.async.commit_group;" ::: "memory"); };
-
-    if (tid < SLOTS) broken[tid] = -1;                   // number of the tile in which a position has no page
+    if (tid == 0) a.desc[blockIdx.x] = make_int4(0, 0, 0, 0);
+    Plan plan{};
+    if (a.planned) plan = make_plan(a, sh.prefix, sh.scan, gridDim.x, blockIdx.x == 0);
+    tc_before();
     __syncthreads();
-    for (int i = 0; i < STAGES; ++i) {
-        const char *k, *v; bool bad;
-        look_up(&k, &v, &bad);
-        put_address(i, k, v, bad);
-        if (lk.unit < lk.end) advance<M>(a, prefix, items, lk, step);
-    }
-    __syncthreads();
-    for (int i = 0; i < STAGES - 1; ++i) {
-        if (ld.unit < ld.end) { load_tile(i, i); advance<M>(a, prefix, items, ld, step); }
-        fence_group();
-    }
+    tc_after();
+    const uint32_t tmem = sh.tmem;
 
-    // ---- state of the group at hand
-    uint32_t qf[KD][4];
-    float acc[DT][4], mx[2], sum[2];
-    int p_row[2];                                        // window: position of this thread's two rows; tree: query number
-    int p_first = 0, p_last = 0;
-    auto begin_group = [&](const Group& g) {
-        const int rows = g.nq * a.group, b = g.item / a.row_tiles;
+    if (role == 2) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+        bool go = true;
+        if (warp == 8) {
+            // ---- keys and values
+            int kvn = 0, tiles_seen = 0;
+            for (int n = 0; go; ++n) {
+                const int si = n % SEGS;
+                if (!(go = warp_wait(smem_at(&sh.seg_full[si]), (n / SEGS) & 1, quit))) break;
+                const Group g = sh.seg[si].g;
+                const int t0 = sh.seg[si].t0, nt = sh.seg[si].t1 - t0;
+                __syncwarp();
+                if (lane == 0) bar_arrive(smem_at(&sh.seg_empty[si]));
+                if (nt <= 0) break;
+                const bool pair = g.rows > TILE_ROWS;
+                for (int o = 0; o < 2 * nt; ++o) {
+                    bool keys; int j;                    // place o of the order: which tile, keys or values
+                    if (pair) { keys = !(o & 1); j = o >> 1; }
+                    else if (o == 0) { keys = true; j = 0; }
+                    else if (o == 2 * nt - 1) { keys = false; j = nt - 1; }
+                    else { keys = o & 1; j = keys ? (o + 1) >> 1 : (o - 2) >> 1; }
+                    const int per = max(a.chunk, 4), x = (t0 + j) * BN + lane * per;     // a lane's entries: drafted or cached together
+                    const bool mine = lane * per < BN;
+                    bool drafted = a.tree && x >= g.axis.n_sink;
+                    int4 rows = make_int4(-BN, -BN, -BN, -BN);           // rows ahead of the map: zeros
+                    if (keys) {
+                        uint32_t bits = 0;
+                        if (a.chunk < 4) {
+                            rows.x = row_of(a, g, x, &drafted); rows.y = row_of(a, g, x + 1, &drafted);
+                            rows.z = row_of(a, g, x + 2, &drafted); rows.w = row_of(a, g, x + 3, &drafted);
+                            bits = (uint32_t)(rows.x >= 0) | (uint32_t)(rows.y >= 0) << 1 | (uint32_t)(rows.z >= 0) << 2 | (uint32_t)(rows.w >= 0) << 3;
+                        } else {
+                            int n_have = 0;              // rows of the chunk that are entries of the axis
+                            const int first = mine ? row_of(a, g, x, &drafted) : -1;
+                            if (first >= 0) { rows.x = first; n_have = min(per, (a.tree && !drafted ? g.len : g.axis.n) - x); }
+                            n_have = __shfl_sync(0xffffffffu, n_have, 4 * lane / per);
+                            bits = below(n_have - 4 * lane % per) & 15u;
+                        }
+                        bits <<= 4 * (lane & 7);
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int r = g.r0 + wm * 16 + lg + 8 * h, qi = r / a.group;
-            const bool there = r < rows;
-            p_row[h] = a.tree ? (there ? qi : -1) : (there ? g.len - g.nq + qi : -1);
-            const T* src = reinterpret_cast<const T*>(a.q) + (int64_t)(g.row0 + (there ? qi : 0)) * a.q_row + (int64_t)(g.head * a.group + (there ? r - qi * a.group : 0)) * a.q_head;
-#pragma unroll
-            for (int kd = 0; kd < KD; ++kd) {
-                qf[kd][h] = there ? __ldg(reinterpret_cast<const uint32_t*>(src + kd * 16 + 2 * lq)) : 0u;
-                qf[kd][2 + h] = there ? __ldg(reinterpret_cast<const uint32_t*>(src + kd * 16 + 8 + 2 * lq)) : 0u;
-            }
-            mx[h] = -INFINITY; sum[h] = 0.f;
-        }
-#pragma unroll
-        for (int d = 0; d < DT; ++d)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) acc[d][e] = 0.f;
-        p_first = g.len - g.nq + g.r0 / a.group;
-        p_last = g.len - g.nq + (min(rows, g.r0 + M) - 1) / a.group;
-        if (a.tree) {                                    // ancestors of every drafted token, as bits; none for one that is not there
-            __syncthreads();
-            if (tid < g.nq) {
-                const int p = a.parents[(int64_t)b * a.max_q + tid];
-                if (p < -2 || p >= tid) atomicExch(a.status, HX_ERR_INVALID_ARG);
-                par[tid] = (p < -2 || p >= tid) ? -2 : p;
-            }
-            __syncthreads();
-            if (tid < g.nq) {
-                uint32_t bits[4] = {0, 0, 0, 0};
-                int t = tid;
-                while (t >= 0) {
-#pragma unroll
-                    for (int w = 0; w < 4; ++w) bits[w] |= (t >> 5) == w ? 1u << (t & 31) : 0u;
-                    t = par[t];
-                }
-                anc[tid] = t == -1 ? make_uint4(bits[0], bits[1], bits[2], bits[3]) : make_uint4(0, 0, 0, 0);
-            }
-            __syncthreads();
-        }
-    };
-
-    bool fresh = true;
-    for (int it = 0; cs.unit < cs.end; ++it) {
-        const int stage = it % STAGES, slot = it % SLOTS;
-        asm volatile("cp.async.wait_group %0;" :: "n"(STAGES - 2) : "memory");
-        __syncthreads();
-        if (ld.unit < ld.end) { load_tile((it + STAGES - 1) % STAGES, (it + STAGES - 1) % SLOTS); advance<M>(a, prefix, items, ld, step); }
-        fence_group();
-        const char *nk, *nv; bool nbad;
-        const bool more = lk.unit < lk.end;
-        look_up(&nk, &nv, &nbad);
-        const Group& g = cs.g;
-        const int tile = cs.tile;
-        if (fresh) { begin_group(g); fresh = false; }
-
-        // scores
-        const uint32_t ks = smem_at(tiles_s + stage * 2 * Shape<D>::TILE), vs = ks + Shape<D>::TILE;
-        float s[NT][4];
-#pragma unroll
-        for (int j = 0; j < NT; ++j)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) s[j][e] = 0.f;
-#pragma unroll
-        for (int kd = 0; kd < KD; ++kd)
-#pragma unroll
-            for (int j = 0; j < NT; j += 2) {
-                uint32_t b[4];
-                const int row = wn * NW + j * 8 + (lane >> 4) * 8 + (lane & 7), c = kd * 2 + ((lane >> 3) & 1);
-                ldsm4(b, ks + piece<D>(row, c));
-                Elem<T>::mma(s[j], qf[kd], b[0], b[1]);
-                Elem<T>::mma(s[j + 1], qf[kd], b[2], b[3]);
-            }
-
-        // masks
-        const int xa = tile * BN, xb = xa + BN - 1;
-        bool whole;
-        if (a.tree) whole = xb < g.axis.n_sink;          // a token that is not there is taken out at the end
-        else whole = hx_window_full(g.axis, xa, xb, p_first, p_last, a.window, a.sinks);
-        whole = whole && broken[slot] != it;
-        if (!whole) {
-            uint4 bits[2];
-#pragma unroll
-            for (int h = 0; h < 2; ++h) bits[h] = (a.tree && p_row[h] >= 0) ? anc[p_row[h]] : make_uint4(0, 0, 0, 0);
-#pragma unroll
-            for (int j = 0; j < NT; ++j)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int h = e >> 1, col = wn * NW + j * 8 + 2 * lq + (e & 1), x = xa + col;
-                    bool see = p_row[h] >= 0 && addr[(slot * 2) * BN + col] != nullptr;
-                    if (a.tree) {
-                        const int t = x - g.axis.n_sink;
-                        const uint4 m = bits[h];
-                        if (t >= 0) { const uint32_t w = t < 32 ? m.x : t < 64 ? m.y : t < 96 ? m.z : m.w; see = see && ((w >> (t & 31)) & 1u); }
-                        else see = see && (m.x | m.y | m.z | m.w);
+                        for (int k = 1; k < 8; k *= 2) bits |= __shfl_xor_sync(0xffffffffu, bits, k);
+                        if ((lane & 7) == 0) sh.valid[(tiles_seen + j) % VALID_RING][lane >> 3] = bits;
+                        sh.rows[(tiles_seen + j) & 3][lane] = rows;
                     } else {
-                        see = see && hx_window_sees(p_row[h], hx_axis_pos(g.axis, x), a.window, a.sinks);
+                        rows = sh.rows[(tiles_seen + j) & 3][lane];          // written by this lane
                     }
-                    if (!see) s[j][e] = -INFINITY;
+                    const int slot = kvn % NS;
+                    const uint32_t bar = smem_at(&sh.full[slot]), to = smem_at(kv_s + slot * S::TILE) + lane * per * 128;
+                    if (!(go = warp_wait(smem_at(&sh.empty[slot]), ((kvn / NS) & 1) ^ 1, quit))) break;
+                    if (lane == 0) bar_expect(bar, S::TILE);
+                    __syncwarp();
+                    const CUtensorMap* map = drafted ? (keys ? &maps.k_draft : &maps.v_draft) : (keys ? &maps.k : &maps.v);
+                    if (mine) {
+#pragma unroll
+                        for (int p = 0; p < S::PANELS; ++p) {
+                            if (a.chunk < 4) gather4(to + p * 16384, map, g.head * D + p * 64, rows, bar);
+                            else load_box(to + p * 16384, map, g.head * D + p * 64, rows.x, bar);
+                        }
+                    }
+                    ++kvn;
                 }
-        }
-
-        // running maximum and sum
-        float alpha[2];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            float m = -INFINITY;
-#pragma unroll
-            for (int j = 0; j < NT; ++j) m = fmaxf(m, fmaxf(s[j][2 * h], s[j][2 * h + 1]));
-            m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 1));
-            m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 2));
-            m = fmaxf(mx[h], m * a.scale_log2);
-            const float safe = m == -INFINITY ? 0.f : m;
-            alpha[h] = exp2_fast(mx[h] - safe);
-            mx[h] = m;
-            float t = 0.f;
-#pragma unroll
-            for (int j = 0; j < NT; ++j)
-#pragma unroll
-                for (int e = 2 * h; e < 2 * h + 2; ++e) { s[j][e] = exp2_fast(__fmaf_rn(s[j][e], a.scale_log2, -safe)); t += s[j][e]; }
-            sum[h] = __fmaf_rn(sum[h], alpha[h], t);
-        }
-#pragma unroll
-        for (int d = 0; d < DT; ++d)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) acc[d][e] *= alpha[e >> 1];
-
-        // weights (rounded to the element type) times values
-        bool odd = false;
-        if (!whole) {                                    // a row that some queries do not see may hold infinities or NaN
-            constexpr int C = Shape<D>::CHUNKS;
-            for (int e = lane; e < NW * C; e += 32) {
-                const int row = wn * NW + e / C, c = e % C;
-                const uint4 x = *reinterpret_cast<const uint4*>(tiles_s + stage * 2 * Shape<D>::TILE + Shape<D>::TILE + piece<D>(row, c));
-                odd = odd || odd_pair<T>(x.x) || odd_pair<T>(x.y) || odd_pair<T>(x.z) || odd_pair<T>(x.w);
+                tiles_seen += nt;
             }
-            odd = __any_sync(0xffffffffu, odd);
-        }
-        uint32_t pf[KT][4];
-#pragma unroll
-        for (int k = 0; k < KT; ++k) {
-            pf[k][0] = Elem<T>::pack(s[2 * k][0], s[2 * k][1]);
-            pf[k][1] = Elem<T>::pack(s[2 * k][2], s[2 * k][3]);
-            pf[k][2] = Elem<T>::pack(s[2 * k + 1][0], s[2 * k + 1][1]);
-            pf[k][3] = Elem<T>::pack(s[2 * k + 1][2], s[2 * k + 1][3]);
-        }
-        if (!odd) {
-#pragma unroll
-            for (int k = 0; k < KT; ++k)
-#pragma unroll
-                for (int d = 0; d < DT; d += 2) {
-                    uint32_t b[4];
-                    const int row = wn * NW + k * 16 + ((lane >> 3) & 1) * 8 + (lane & 7), c = d + (lane >> 4);
-                    ldsm4t(b, vs + piece<D>(row, c));
-                    Elem<T>::mma(acc[d], pf[k], b[0], b[1]);
-                    Elem<T>::mma(acc[d + 1], pf[k], b[2], b[3]);
-                }
+            // copies that are on their way end before the block does
+            for (int i = 0; i < NS && !go; ++i) {
+                const int at = kvn - 1 - i;
+                if (at >= 0) { const unsigned long long t0 = now_ns(); while (!bar_try(smem_at(&sh.full[at % NS]), (at / NS) & 1) && now_ns() - t0 < WAIT_NS) { } }
+            }
         } else {
-            // finite values as always; of the others, how many of each kind a query sees (with a weight above zero)
-            uint32_t seen[KT][4];
-#pragma unroll
-            for (int k = 0; k < KT; ++k)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const float* w = s[2 * k + (r >> 1)] + 2 * (r & 1);
-                    seen[k][r] = (w[0] > 0.f ? Elem<T>::ONE : 0u) | (w[1] > 0.f ? Elem<T>::ONE << 16 : 0u);
-                }
-#pragma unroll
-            for (int d = 0; d < DT; d += 2) {
-                float kinds[2][3][4] = {};
-                for (int k = 0; k < KT; ++k) {
-                    uint32_t b[4], fin[4], plus[4], minus[4], nan[4], p4[4], s4[4];
-#pragma unroll
-                    for (int kk = 0; kk < KT; ++kk)      // registers cannot be indexed by k
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) if (kk == k) { p4[r] = pf[kk][r]; s4[r] = seen[kk][r]; }
-                    const int row = wn * NW + k * 16 + ((lane >> 3) & 1) * 8 + (lane & 7), c = d + (lane >> 4);
-                    ldsm4t(b, vs + piece<D>(row, c));
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) split_pair<T>(b[r], fin[r], plus[r], minus[r], nan[r]);
-#pragma unroll
-                    for (int o = 0; o < 2; ++o) {
-                        Elem<T>::mma(acc[d + o], p4, fin[2 * o], fin[2 * o + 1]);
-                        Elem<T>::mma(kinds[o][0], s4, plus[2 * o], plus[2 * o + 1]);
-                        Elem<T>::mma(kinds[o][1], s4, minus[2 * o], minus[2 * o + 1]);
-                        Elem<T>::mma(kinds[o][2], s4, nan[2 * o], nan[2 * o + 1]);
+            // ---- rows of q
+            for (int n = 0; go; ++n) {
+                const int si = n % SEGS;
+                if (!(go = warp_wait(smem_at(&sh.seg_full[si]), (n / SEGS) & 1, quit))) break;
+                const Seg& seg = sh.seg[si];
+                const int rows = seg.g.rows, r0 = seg.g.r0, row0 = seg.g.row0, head0 = seg.g.head * a.group, nt = seg.t1 - seg.t0;
+                __syncwarp();
+                if (lane == 0) bar_arrive(smem_at(&sh.seg_empty[si]));
+                if (nt <= 0) break;
+                if (!(go = warp_wait(smem_at(&sh.q_empty), (n & 1) ^ 1, quit))) break;
+                for (int rb = (warp - 9) * 32; rb < rows; rb += 96) {        // 32 rows, a lane finds the place of each
+                    const int r = rb + lane;
+                    const int qi = r < rows ? (r0 + r) / a.group : 0, hd = r < rows ? r0 + r - qi * a.group : 0;
+                    const unsigned long long src = reinterpret_cast<unsigned long long>(a.q + 2 * ((int64_t)(row0 + qi) * a.q_row + (int64_t)(head0 + hd) * a.q_head));
+#pragma unroll 4
+                    for (int i = 0; i < S::CHUNKS; ++i) {
+                        const int e = i * 32 + lane, q = e / S::CHUNKS, c = e - q * S::CHUNKS, rr = rb + q;
+                        const char* from = reinterpret_cast<const char*>(__shfl_sync(0xffffffffu, src, q));
+                        copy16(smem_at(q_s + (rr >> 7) * S::TILE) + piece(rr & 127, c), from + c * 16, rr < rows ? 16 : 0);
                     }
                 }
-#pragma unroll
-                for (int o = 0; o < 2; ++o)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        if (kinds[o][0][e] > 0.f) acc[d + o][e] += INFINITY;
-                        if (kinds[o][1][e] > 0.f) acc[d + o][e] -= INFINITY;
-                        if (kinds[o][2][e] > 0.f) acc[d + o][e] = __int_as_float(0x7fffffff);
-                    }
+                copies_wait();
+                fence_async();
+                bar_arrive(smem_at(&sh.q_full));
             }
         }
-
-        const bool ends = tile + 1 == g.tiles || (a.planned && cs.unit + 1 == cs.end);
-        if (ends) {
-            // ---- end of the group, or of this block's part of it
-            const bool begun_here = !a.planned || cs.unit - tile >= first_unit;
-            const bool complete = begun_here && tile + 1 == g.tiles;
+    } else if (role == 3) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+        if (warp == 12) {
+            // ---- products
+            constexpr uint32_t QK = product(Elem<T>::FORMAT, BN, false), PV = product(Elem<T>::FORMAT, D, true);
+            const uint64_t q_m = matrix(smem_at(q_s), 16), k_m = matrix(smem_at(kv_s), 16), v_m = matrix(smem_at(kv_s), 16384);
+            int kvn = 0, pn[2] = {0, 0};
+            bool go = true;
+            for (int n = 0; go; ++n) {
+                const int si = n % SEGS;
+                if (!(go = warp_wait(smem_at(&sh.seg_full[si]), (n / SEGS) & 1, quit))) break;
+                const int nt = sh.seg[si].t1 - sh.seg[si].t0;
+                const bool pair = sh.seg[si].g.rows > TILE_ROWS;
+                __syncwarp();
+                if (lane == 0) bar_arrive(smem_at(&sh.seg_empty[si]));
+                if (nt <= 0) break;
+                // scores of tile j for stream s; last: the last reader of the keys; done: the last products that read q
+                auto scores = [&](int s, int j, bool last, bool done) {
+                    const int at = kvn + key_place(pair, nt, j), slot = at % NS;
+                    if (!warp_wait(smem_at(&sh.full[slot]), (at / NS) & 1, quit)) return false;
+                    tc_after();
+                    if (elect()) {
+                        const uint64_t kt = k_m + (uint64_t)(slot * (S::TILE >> 4)), qt = q_m + (uint64_t)((pair ? s : 0) * (S::TILE >> 4));
+                        const uint32_t to = tmem + s * 128;
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                sum[h] += __shfl_xor_sync(0xffffffffu, sum[h], 1);
-                sum[h] += __shfl_xor_sync(0xffffffffu, sum[h], 2);
-                if (a.tree) {
-                    const uint4 m = p_row[h] >= 0 ? anc[p_row[h]] : make_uint4(0, 0, 0, 0);
-                    if (!(m.x | m.y | m.z | m.w)) {      // no such token
-                        mx[h] = -INFINITY; sum[h] = 0.f;
-#pragma unroll
-                        for (int d = 0; d < DT; ++d) acc[d][2 * h] = acc[d][2 * h + 1] = 0.f;
+                        for (int ks = 0; ks < D / 16; ++ks)
+                            tc_mma_ss(to, qt + (uint64_t)((ks >> 2) * 1024 + (ks & 3) * 2), kt + (uint64_t)((ks >> 2) * 1024 + (ks & 3) * 2), QK, ks > 0);
+                        tc_commit(smem_at(&sh.s_full[s]));
+                        if (last) tc_commit(smem_at(&sh.empty[slot]));
+                        if (done) tc_commit(smem_at(&sh.q_empty));
                     }
-                }
-            }
-            if constexpr (WN > 1) {                      // the warps' tokens joined, in the order of the warps, where the tile was
-                float* join = reinterpret_cast<float*>(tiles_s + stage * 2 * Shape<D>::TILE);
-                float* stat = join + 16 * Shape<D>::OPITCH;
-                static_assert(16 * Shape<D>::OPITCH * 4 + 4 * 16 * 2 * 4 <= 2 * Shape<D>::TILE, "joining buffer");
-                __syncthreads();
-                if (lq == 0) {
+                    __syncwarp();
+                    return true;
+                };
+                // weights of tile j times its values, for stream s; end: the stream's last tile of the group
+                auto values = [&](int s, int j, bool first, bool last, bool end) {
+                    const int at = kvn + value_place(pair, nt, j), slot = at % NS;
+                    if (!warp_wait(smem_at(&sh.full[slot]), (at / NS) & 1, quit)) return false;
+                    if (!warp_wait(smem_at(&sh.p_full[s]), pn[s] & 1, quit)) return false;
+                    ++pn[s];
+                    tc_after();
+                    if (elect()) {
+                        const uint64_t vt = v_m + (uint64_t)(slot * (S::TILE >> 4));
+                        const uint32_t from = tmem + s * 128, to = tmem + 256 + s * 128;
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) { stat[(wn * 16 + lg + 8 * h) * 2] = mx[h]; stat[(wn * 16 + lg + 8 * h) * 2 + 1] = sum[h]; }
-                }
-                __syncthreads();
-                float f[2];
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    float m = -INFINITY, t = 0.f;
-#pragma unroll
-                    for (int w = 0; w < WN; ++w) m = fmaxf(m, stat[(w * 16 + lg + 8 * h) * 2]);
-                    const float safe = m == -INFINITY ? 0.f : m;
-#pragma unroll
-                    for (int w = 0; w < WN; ++w) t = __fmaf_rn(stat[(w * 16 + lg + 8 * h) * 2 + 1], exp2_fast(stat[(w * 16 + lg + 8 * h) * 2] - safe), t);
-                    f[h] = exp2_fast(mx[h] - safe);
-                    mx[h] = m; sum[h] = t;
-                }
-                for (int w = 0; w < WN; ++w) {
-                    if (w == wn) {
-#pragma unroll
-                        for (int d = 0; d < DT; ++d)
-#pragma unroll
-                            for (int h = 0; h < 2; ++h) {
-                                float2* o = reinterpret_cast<float2*>(join + (lg + 8 * h) * Shape<D>::OPITCH + d * 8 + 2 * lq);
-                                float2 x = w ? *o : make_float2(0.f, 0.f);
-                                x.x = __fmaf_rn(acc[d][2 * h], f[h], x.x); x.y = __fmaf_rn(acc[d][2 * h + 1], f[h], x.y);
-                                *o = x;
-                            }
+                        for (int ks = 0; ks < BN / 16; ++ks) tc_mma_ts(to, from + ks * 8, vt + (uint64_t)(ks * 128), PV, !(first && ks == 0));
+                        if (last) tc_commit(smem_at(&sh.empty[slot]));
+                        if (end) tc_commit(smem_at(&sh.o_full[s]));
                     }
-                    __syncthreads();
-                }
-                // every warp takes a quarter of the columns
-#pragma unroll
-                for (int d = 0; d < DT; ++d)
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const float2 x = *reinterpret_cast<const float2*>(join + (lg + 8 * h) * Shape<D>::OPITCH + d * 8 + 2 * lq);
-                        acc[d][2 * h] = x.x; acc[d][2 * h + 1] = x.y;
+                    __syncwarp();
+                    return true;
+                };
+                if (!(go = warp_wait(smem_at(&sh.q_full), n & 1, quit))) break;
+                if (pair) {
+                    go = scores(0, 0, false, false) && scores(1, 0, true, nt == 1);
+                    for (int j = 0; j < nt && go; ++j) {
+                        const bool end = j + 1 == nt;
+                        go = values(0, j, j == 0, false, end) && (end || scores(0, j + 1, false, false)) && values(1, j, j == 0, true, end) &&
+                             (end || scores(1, j + 1, true, j + 2 == nt));
                     }
-            }
-            const int rows = g.nq * a.group;
-            float* part = nullptr;
-            if (!complete) part = a.part + ((int64_t)blockIdx.x * 2 + (cs.unit - tile <= first_unit ? 0 : 1)) * M * (D + 2);
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int rr = wm * 16 + lg + 8 * h, r = g.r0 + rr;
-                if (r >= rows) continue;
-                if (complete) {
-                    const int qi = r / a.group, head = g.head * a.group + r - qi * a.group;
-                    const float inv = sum[h] > 0.f ? __fdividef(1.f, sum[h]) : (sum[h] == 0.f ? 0.f : sum[h]);
-                    T* o = reinterpret_cast<T*>(a.out) + (int64_t)(g.row0 + qi) * a.o_row + (int64_t)head * a.o_head;
-#pragma unroll
-                    for (int d = 0; d < DT; ++d)
-                        if (WN == 1 || d % WN == wn) *reinterpret_cast<uint32_t*>(o + d * 8 + 2 * lq) = Elem<T>::pack(acc[d][2 * h] * inv, acc[d][2 * h + 1] * inv);
-                    if (a.lse && lq == 0 && wn == 0)
-                        a.lse[(int64_t)(g.row0 + qi) * a.n_kv_heads * a.group + head] = sum[h] == 0.f ? -INFINITY : __fmaf_rn(mx[h], LN2, logf(sum[h]));
                 } else {
-                    float* o = part + (int64_t)rr * (D + 2);
-#pragma unroll
-                    for (int d = 0; d < DT; ++d)
-                        if (WN == 1 || d % WN == wn) *reinterpret_cast<float2*>(o + 2 + d * 8 + 2 * lq) = make_float2(acc[d][2 * h], acc[d][2 * h + 1]);
-                    if (lq == 0 && wn == 0) { o[0] = mx[h]; o[1] = sum[h]; }
+                    go = scores(0, 0, true, nt == 1) && (nt < 2 || scores(1, 1, true, nt == 2));
+                    for (int j = 0; j < nt && go; ++j)
+                        go = values(j & 1, j, j < 2, true, j + 2 >= nt) && (j + 2 >= nt || scores(j & 1, j + 2, true, j + 3 == nt));
                 }
+                kvn += 2 * nt;
             }
-            if (!complete && begun_here && tid == 0) {   // the shares that hold the rest of the group follow this one
-                const int64_t last = cs.unit - tile + g.tiles - 1;
-                a.desc[blockIdx.x] = make_int4(hx_share_of(total, last, shares) - (int)blockIdx.x + 1, g.item, g.head, cs.unit - tile <= first_unit ? 0 : 1);
+            if (!go) {                                   // what was issued ends before the tensor memory is given back
+                if (elect()) tc_commit(smem_at(&sh.drained));
+                __syncwarp();
+                const unsigned long long t0 = now_ns();
+                while (!bar_try(smem_at(&sh.drained), 0) && now_ns() - t0 < WAIT_NS) { }
             }
-            fresh = true;
+        } else if (warp == 13) {
+            // ---- groups
+            Walk w = begin_walk(a, plan, blockIdx.x, gridDim.x);
+            for (int n = 0;; ++n) {
+                Group g;
+                int t0 = 0, t1 = 0;
+                int64_t start = 0;
+                const bool more = next_group(a, sh.prefix, w, &g, &t0, &t1, &start);
+                const int si = n % SEGS;
+                if (!warp_wait(smem_at(&sh.seg_empty[si]), ((n / SEGS) & 1) ^ 1, quit)) break;
+                Seg& seg = sh.seg[si];
+                if (more && a.tree) ancestors(a, g.item / a.row_tiles, seg.anc, sh.link);
+                if (lane == 0) {
+                    if (more) seg.g = g;
+                    seg.t0 = more ? t0 : 0; seg.t1 = more ? t1 : 0;
+                    if (more && a.planned && t0 == 0 && t1 < g.tiles)        // the shares that hold the rest of the group follow this one
+                        a.desc[blockIdx.x] = make_int4(hx_share_of(plan.total, start + g.tiles - 1, plan.shares) - (int)blockIdx.x + 1, g.item, g.head, 0);
+                }
+                __syncwarp();
+                if (lane == 0) bar_arrive(smem_at(&sh.seg_full[si]));
+                if (!more) break;
+            }
         }
-        advance<M>(a, prefix, items, cs, step);
-        put_address(it + STAGES, nk, nv, nbad);          // loaded in the next iteration, behind its barrier
-        if (more) advance<M>(a, prefix, items, lk, step);
+    } else {
+        // ---- softmax
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 192;");
+        const int s = role, row = tid & 127;
+        const uint32_t lanes = (uint32_t)(warp & 3) << 21;       // the warp's quarter of the 128 lanes
+        const uint32_t S_at = tmem + lanes + s * 128, O_at = tmem + lanes + 256;
+        int sn = 0, on[2] = {0, 0}, xn = 0, kvn = 0, tiles_seen = 0;
+        bool go = true, odd = false;
+        for (int n = 0; go; ++n) {
+            const int si = n % SEGS;
+            if (!(go = warp_wait(smem_at(&sh.seg_full[si]), (n / SEGS) & 1, quit))) break;
+            const Seg& seg = sh.seg[si];
+            const int t0 = seg.t0, nt = seg.t1 - t0;
+            if (nt <= 0) break;
+            const Group& g = seg.g;
+            const bool pair = g.rows > TILE_ROWS;
+            const int r = row + (pair ? s * TILE_ROWS : 0);      // row of the group
+            const bool live = (warp & 3) * 32 + (pair ? s * TILE_ROWS : 0) < g.rows;     // the warp has rows
+            const bool there = r < g.rows;
+            int p_first = 0, p_last = 0;
+            if (!a.tree) {
+                p_first = g.len - g.nq + (g.r0 + (pair ? s * TILE_ROWS : 0)) / a.group;
+                p_last = g.len - g.nq + (g.r0 + min(g.rows, (pair ? s + 1 : 1) * TILE_ROWS) - 1) / a.group;
+            }
+            float mx = -INFINITY, sum = 0.f;
+            for (int j = pair ? 0 : s; j < nt; j += pair ? 1 : 2) {
+                if (!(go = warp_wait(smem_at(&sh.s_full[s]), sn & 1, quit))) break;
+                ++sn;
+                tc_after();
+                const int xa = (t0 + j) * BN;
+                bool whole = a.tree ? xa + BN <= g.axis.n_sink : hx_window_full(g.axis, xa, xa + BN - 1, p_first, p_last, a.window, a.sinks);
+                const uint4 valid = *reinterpret_cast<const uint4*>(sh.valid[(tiles_seen + j) % VALID_RING]);
+                whole = whole && (valid.x & valid.y & valid.z & valid.w) == 0xffffffffu;
+                if (!whole) {                            // a value that some rows do not see may be infinite or NaN
+                    const int at = kvn + value_place(pair, nt, j), slot = at % NS;
+                    if (!(go = warp_wait(smem_at(&sh.full[slot]), (at / NS) & 1, quit))) break;
+                    char* tile = kv_s + slot * S::TILE;
+                    const uint32_t word = row < 32 ? valid.x : row < 64 ? valid.y : row < 96 ? valid.z : valid.w;
+                    if ((word >> lane) & 1) {
+                        for (int c = 0; c < S::CHUNKS; ++c) {
+                            const uint4 x = *reinterpret_cast<const uint4*>(tile + piece(row, c));
+                            const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+                            for (int i = 0; i < 4; ++i)
+                                odd = odd || (w[i] & Elem<T>::EXP) == Elem<T>::EXP || (w[i] & (Elem<T>::EXP << 16)) == (Elem<T>::EXP << 16);
+                        }
+                    } else {                             // no entry of the axis: rows behind the end of a page's use hold anything
+                        for (int c = 0; c < S::CHUNKS; ++c) *reinterpret_cast<uint4*>(tile + piece(row, c)) = make_uint4(0, 0, 0, 0);
+                        fence_async();
+                    }
+                }
+                if (live) {
+                    uint32_t x[128];
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) tc_ld32(x + 32 * c, S_at + 32 * c);
+                    tc_ld_wait();
+                    if (!whole) {
+                        uint32_t m[4] = {0, 0, 0, 0};
+                        if (there) sees(a, g, seg.anc, r, xa, m);
+                        m[0] &= valid.x; m[1] &= valid.y; m[2] &= valid.z; m[3] &= valid.w;
+#pragma unroll
+                        for (int i = 0; i < 128; ++i) if (!((m[i >> 5] >> (i & 31)) & 1)) x[i] = 0xff800000u;
+                    }
+                    float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                    for (int i = 0; i < 128; i += 8)
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) m4[k] = fmaxf(fmaxf(m4[k], __uint_as_float(x[i + k])), __uint_as_float(x[i + 4 + k]));
+                    const float top = fmaxf(mx, fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * a.scale_log2);
+                    const bool first = j < (pair ? 1 : 2);
+                    if (__any_sync(0xffffffffu, top > mx + GROWTH || (first && top != mx))) {
+                        const float alpha = top == mx ? 1.f : exp2_fast(mx - top);       // mx < top: finite or zero
+                        mx = top; sum *= alpha;
+                        if (!first) {
+#pragma unroll
+                            for (int c = 0; c < D; c += 16) {
+                                uint32_t o[16];
+                                tc_ld16(o, O_at + s * 128 + c);
+                                tc_ld_wait();
+#pragma unroll
+                                for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * alpha);
+                                tc_st16(O_at + s * 128 + c, o);
+                            }
+                        }
+                    }
+                    const float safe = mx == -INFINITY ? 0.f : mx;
+                    float s4[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) {
+                        uint32_t w[8];
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            const float u = exp2_fast(__fmaf_rn(__uint_as_float(x[16 * c + 2 * i]), a.scale_log2, -safe));
+                            const float v = exp2_fast(__fmaf_rn(__uint_as_float(x[16 * c + 2 * i + 1]), a.scale_log2, -safe));
+                            s4[(2 * i) & 3] += u; s4[(2 * i + 1) & 3] += v;
+                            w[i] = Elem<T>::pack(u, v);
+                        }
+                        tc_st8(S_at + 8 * c, w);
+                    }
+                    sum += (s4[0] + s4[1]) + (s4[2] + s4[3]);
+                    tc_st_wait();
+                }
+                tc_before();
+                __syncwarp();
+                if (lane == 0) bar_arrive(smem_at(&sh.p_full[s]));
+            }
+            if (!go) break;
+
+            // ---- end of the group, or of this block's part of it
+            const bool both = !pair && nt > 1;           // the second stream has half of the tiles of the same rows
+            if (a.tree && there) {
+                const uint4 m = seg.anc[(g.r0 + r) / a.group];
+                if (!(m.x | m.y | m.z | m.w)) { mx = -INFINITY; sum = 0.f; }
+            }
+            if (both && s == 1) {
+                sh.stat[row] = make_float2(mx, sum);
+                __syncwarp();
+                if (lane == 0) bar_arrive(smem_at(&sh.x_ready));
+                if (!(go = warp_wait(smem_at(&sh.x_free), xn & 1, quit))) break;
+                ++xn;
+            } else if (pair || s == 0) {
+                if (!(go = warp_wait(smem_at(&sh.o_full[s]), on[s] & 1, quit))) break;
+                ++on[s];
+                float f0 = 1.f, f1 = 0.f;
+                if (both) {
+                    if (!(go = warp_wait(smem_at(&sh.o_full[1]), on[1] & 1, quit))) break;
+                    ++on[1];
+                    if (!(go = warp_wait(smem_at(&sh.x_ready), xn & 1, quit))) break;
+                    ++xn;
+                    const float2 o = sh.stat[row];
+                    const float m = fmaxf(mx, o.x), safe = m == -INFINITY ? 0.f : m;
+                    f0 = exp2_fast(mx - safe); f1 = exp2_fast(o.x - safe);
+                    sum = __fmaf_rn(sum, f0, o.y * f1); mx = m;
+                }
+                tc_after();
+                const bool complete = t0 == 0 && seg.t1 == g.tiles;
+                const bool none = sum == 0.f;            // sees nothing here: what the products left says nothing
+                const float inv = none ? 0.f : 1.f / sum;
+                const int qi = (g.r0 + r) / a.group, head = g.head * a.group + g.r0 + r - qi * a.group;
+                T* out = reinterpret_cast<T*>(a.out) + (int64_t)(g.row0 + qi) * a.o_row + (int64_t)head * a.o_head;
+                float* part = a.part + (((int64_t)blockIdx.x * 2 + (t0 > 0 ? 0 : 1)) * GROUP_ROWS + r) * (D + 4);
+                if (live) {
+#pragma unroll
+                    for (int c = 0; c < D; c += 32) {
+                        uint32_t o[32], p[32];
+                        tc_ld32(o, O_at + s * 128 + c);
+                        if (both) tc_ld32(p, O_at + 128 + c);
+                        tc_ld_wait();
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) {
+                            float x = __uint_as_float(o[i]);
+                            if (both) x = (f0 == 0.f ? 0.f : x * f0) + (f1 == 0.f ? 0.f : __uint_as_float(p[i]) * f1);
+                            o[i] = __float_as_uint(none ? 0.f : x);
+                        }
+                        if (there && complete) {
+                            uint32_t w[16];
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) w[i] = Elem<T>::pack(__uint_as_float(o[2 * i]) * inv, __uint_as_float(o[2 * i + 1]) * inv);
+                            if (a.out16) {
+#pragma unroll
+                                for (int i = 0; i < 4; ++i) reinterpret_cast<uint4*>(out + c)[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+                            } else {
+#pragma unroll
+                                for (int i = 0; i < 16; ++i) reinterpret_cast<uint32_t*>(out + c)[i] = w[i];
+                            }
+                        } else if (there) {
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) reinterpret_cast<uint4*>(part + 4 + c)[i] = make_uint4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+                        }
+                    }
+                    if (there) {
+                        if (!complete) *reinterpret_cast<float2*>(part) = make_float2(mx, sum);
+                        else if (a.lse) a.lse[(int64_t)(g.row0 + qi) * a.n_kv_heads * a.group + head] = none ? -INFINITY : __fmaf_rn(mx, LN2, logf(sum));
+                    }
+                }
+                tc_before();
+                __syncwarp();
+                if (both && lane == 0) bar_arrive(smem_at(&sh.x_free));
+            }
+            // the stream that had no tile, or whose rows the first one has written, has nothing to wait for
+            if (s == 1 && !pair) { if (both) ++on[1]; }
+            if (s == 0 && pair) ++on[1];
+            __syncwarp();
+            if (lane == 0) bar_arrive(smem_at(&sh.seg_empty[si]));
+            kvn += 2 * nt;
+            tiles_seen += nt;
+        }
+        if (__any_sync(0xffffffffu, odd) && lane == 0) reinterpret_cast<volatile int4*>(a.desc)[blockIdx.x].w = 1;
     }
+    __syncwarp();
+    tc_before();
+    __syncthreads();
+    tc_after();
+    if (warp == 0) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" :: "r"(tmem) : "memory");
+    if (tid == 0 && sh.quit) atomicExch(a.status, HX_ERR_TIMEOUT);
 }
 
-// Joins the parts of the groups that begin in a share and end in another, in the order of the shares.
-template <int D, int M, class T>
-__global__ void __launch_bounds__(THREADS) hx_attend_join_kernel(const AttendArgs a) {
+// One row of a group by one warp, reading what the row sees and nothing else.
+template <int D, class T>
+__device__ void one_row(const AttendArgs& a, const Group& g, const uint4* anc, int r) {
+    const int lane = threadIdx.x & 31, qi = (g.r0 + r) / a.group, head = g.head * a.group + g.r0 + r - qi * a.group;
+    const uint32_t* q = reinterpret_cast<const uint32_t*>(a.q + 2 * ((int64_t)(g.row0 + qi) * a.q_row + (int64_t)head * a.q_head));
+    float m = -INFINITY, l = 0.f, acc[D / 32];
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) acc[i] = 0.f;
+    for (int x0 = 0; x0 < g.axis.n; x0 += 32) {
+        uint32_t bits[4];
+        sees(a, g, anc, r, x0, bits);
+        bool drafted;
+        const int at = row_of(a, g, x0 + lane, &drafted);
+        const bool see = at >= 0 && ((bits[0] >> lane) & 1);
+        const int64_t byte = (int64_t)at * (drafted ? a.draft_row_bytes : (int64_t)a.token_bytes) + (int64_t)g.head * (D * 2);
+        const char *k = (drafted ? a.k_draft : a.k) + byte, *v = (drafted ? a.v_draft : a.v) + byte;
+        float s = -INFINITY;
+        if (see) {
+            s = 0.f;
+            for (int i = 0; i < D / 2; ++i) {
+                const float2 x = Elem<T>::unpack(reinterpret_cast<const uint32_t*>(k)[i]), y = Elem<T>::unpack(q[i]);
+                s = __fmaf_rn(x.x, y.x, s); s = __fmaf_rn(x.y, y.y, s);
+            }
+            s *= a.scale_log2;
+        }
+        float t = s;
+#pragma unroll
+        for (int o = 16; o; o >>= 1) t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, o));
+        const float mn = fmaxf(m, t), safe = mn == -INFINITY ? 0.f : mn, alpha = exp2_fast(m - safe);
+        float p = see ? exp2_fast(s - safe) : 0.f;
+        m = mn;
+        float ps = p;
+#pragma unroll
+        for (int o = 16; o; o >>= 1) ps += __shfl_xor_sync(0xffffffffu, ps, o);
+        l = __fmaf_rn(l, alpha, ps);
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) acc[i] *= alpha;
+        for (uint32_t todo = __ballot_sync(0xffffffffu, see); todo; todo &= todo - 1) {
+            const int j = __ffs(todo) - 1;
+            const float w = __shfl_sync(0xffffffffu, p, j);
+            const T* row = reinterpret_cast<const T*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(v), j));
+#pragma unroll
+            for (int i = 0; i < D / 32; ++i) acc[i] = __fmaf_rn(w, (float)row[i * 32 + lane], acc[i]);
+        }
+    }
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    T* out = reinterpret_cast<T*>(a.out) + (int64_t)(g.row0 + qi) * a.o_row + (int64_t)head * a.o_head;
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) out[i * 32 + lane] = T(l == 0.f ? 0.f : acc[i] * inv);
+    if (a.lse && lane == 0) a.lse[(int64_t)(g.row0 + qi) * a.n_kv_heads * a.group + head] = l == 0.f ? -INFINITY : __fmaf_rn(m, LN2, logf(l));
+}
+
+constexpr int JOIN_THREADS = 256;
+
+// Joins the parts of the groups that begin in a share and end in another, in the order of the shares; computes the groups of a
+// block again that found infinities or NaN where some rows do not look.
+template <int D, class T>
+__global__ void __launch_bounds__(JOIN_THREADS) hx_attend_join_kernel(const AttendArgs a) {
     hx_wait_for_primary();
+    __shared__ int64_t prefix[PLAN_ITEMS + 1], scan[JOIN_THREADS / 32];
+    __shared__ uint4 anc[HX_TREE_MAX];
+    __shared__ int link[HX_TREE_MAX];
     const int4 de = a.desc[blockIdx.x];
+    const int tid = threadIdx.x;
+    if (de.w) {
+        Plan plan{};
+        if (a.planned) plan = make_plan(a, prefix, scan, gridDim.x, false);
+        Walk w = begin_walk(a, plan, blockIdx.x, gridDim.x);
+        Group g;
+        int t0, t1;
+        int64_t start;
+        while (next_group(a, prefix, w, &g, &t0, &t1, &start)) {
+            __syncthreads();
+            if (a.tree && tid < 32) ancestors(a, g.item / a.row_tiles, anc, link);
+            __syncthreads();
+            for (int r = tid >> 5; r < g.rows; r += JOIN_THREADS / 32) one_row<D, T>(a, g, anc, r);
+        }
+    }
     if (de.x == 0) return;
-    const Group g = group_of<M>(a, de.y, de.z);
-    const int rows = min(M, g.nq * a.group - g.r0), tid = threadIdx.x;
+    for (int i = 0; i < de.x; ++i) if (a.desc[blockIdx.x + i].w) return;     // that block has computed the group whole
+    const Group g = group_of(a, de.y, de.z);
     constexpr int PER = D / 4;                           // four elements to a thread
-    for (int e = tid; e < rows * PER; e += THREADS) {
-        const int rr = e / PER, c = (e - rr * PER) * 4;
-        float m = -INFINITY, l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int e = tid; e < g.rows * PER; e += JOIN_THREADS) {
+        const int r = e / PER, c = (e - r * PER) * 4;
+        float m = -INFINITY, l = 0.f;
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
         for (int i = 0; i < de.x; ++i) {
-            const float* p = a.part + ((int64_t)(blockIdx.x + i) * 2 + (i ? 0 : de.w)) * M * (D + 2) + (int64_t)rr * (D + 2);
+            const float* p = a.part + (((int64_t)(blockIdx.x + i) * 2 + (i ? 0 : 1)) * GROUP_ROWS + r) * (D + 4);
             const float2 st = *reinterpret_cast<const float2*>(p);
             const float mn = fmaxf(m, st.x), safe = mn == -INFINITY ? 0.f : mn, fo = exp2_fast(m - safe), fn = exp2_fast(st.x - safe);
-            const float2 x = *reinterpret_cast<const float2*>(p + 2 + c), y = *reinterpret_cast<const float2*>(p + 4 + c);
+            const float4 x = *reinterpret_cast<const float4*>(p + 4 + c);
             l = __fmaf_rn(l, fo, st.y * fn);
-            o[0] = __fmaf_rn(o[0], fo, x.x * fn); o[1] = __fmaf_rn(o[1], fo, x.y * fn);
-            o[2] = __fmaf_rn(o[2], fo, y.x * fn); o[3] = __fmaf_rn(o[3], fo, y.y * fn);
+            o.x = __fmaf_rn(o.x, fo, x.x * fn); o.y = __fmaf_rn(o.y, fo, x.y * fn);
+            o.z = __fmaf_rn(o.z, fo, x.z * fn); o.w = __fmaf_rn(o.w, fo, x.w * fn);
             m = mn;
         }
-        const int r = g.r0 + rr, qi = r / a.group, head = g.head * a.group + r - qi * a.group;
-        const float inv = l > 0.f ? __fdividef(1.f, l) : (l == 0.f ? 0.f : l);
-        T* to = reinterpret_cast<T*>(a.out) + (int64_t)(g.row0 + qi) * a.o_row + (int64_t)head * a.o_head + c;
-        reinterpret_cast<uint32_t*>(to)[0] = Elem<T>::pack(o[0] * inv, o[1] * inv);
-        reinterpret_cast<uint32_t*>(to)[1] = Elem<T>::pack(o[2] * inv, o[3] * inv);
+        const int qi = (g.r0 + r) / a.group, head = g.head * a.group + g.r0 + r - qi * a.group;
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        uint32_t* to = reinterpret_cast<uint32_t*>(reinterpret_cast<T*>(a.out) + (int64_t)(g.row0 + qi) * a.o_row + (int64_t)head * a.o_head + c);
+        to[0] = Elem<T>::pack(o.x * inv, o.y * inv);
+        to[1] = Elem<T>::pack(o.z * inv, o.w * inv);
         if (c == 0 && a.lse) a.lse[(int64_t)(g.row0 + qi) * a.n_kv_heads * a.group + head] = l == 0.f ? -INFINITY : __fmaf_rn(m, LN2, logf(l));
     }
 }
 
-constexpr int MAX_BLOCKS = 296;      // two to each of 148 multiprocessors
-size_t part_bytes(int D, int M) { return (size_t)MAX_BLOCKS * 2 * M * (D + 2) * sizeof(float); }
+constexpr int MAX_BLOCKS = 148;      // one to each multiprocessor
 
-template <int D, int WM, class T>
-cudaError_t launch(const HxCore& core, AttendArgs a, size_t* allowed, cudaStream_t s) {
-    constexpr int M = 16 * WM;
-    a.row_tiles = hx_ceil_div(a.max_q * a.group, M);
-    const int64_t items = (int64_t)a.n * a.row_tiles;
-    a.planned = items <= PLAN_ITEMS;
-    cudaError_t e = hx_opt_in_smem(hx_attend_kernel<D, WM, T>, smem_bytes<D>(), allowed, 48 * 1024);
-    if (e != cudaSuccess) return e;
-    const int blocks = std::min(2 * core.n_sm, MAX_BLOCKS);
-    e = hx_launch_dependent(hx_attend_kernel<D, WM, T>, dim3(blocks), dim3(THREADS), smem_bytes<D>(), s, a);
-    if (e != cudaSuccess) return e;
-    ++*core.launches;
-    if (!a.planned) return cudaSuccess;
-    e = hx_launch_dependent(hx_attend_join_kernel<D, M, T>, dim3(blocks), dim3(THREADS), 0, s, a);
-    if (e == cudaSuccess) ++*core.launches;
-    return e;
+size_t part_bytes(int D) { return (size_t)MAX_BLOCKS * 2 * GROUP_ROWS * (D + 4) * sizeof(float); }
+
+typedef CUresult (*EncodeTiled)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*, const cuuint32_t*,
+                                CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+EncodeTiled encoder() {              // through the runtime, so that the library need not be linked against the driver
+    static EncodeTiled f = [] {
+        void* p = nullptr;
+        cudaDriverEntryPointQueryResult found;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &found) != cudaSuccess || found != cudaDriverEntryPointSuccess) p = nullptr;
+        return reinterpret_cast<EncodeTiled>(p);
+    }();
+    return f;
+}
+
+// Rows of `width` elements, `pitch` bytes apart, read `together` rows of 64 elements at a time (one for a gather) into swizzled rows of
+// 128 bytes.
+template <class T>
+bool encode(CUtensorMap* map, const char* base, int64_t width, int64_t rows, int64_t pitch, int together) {
+    const cuuint64_t dims[2] = {(cuuint64_t)width, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)pitch};
+    const cuuint32_t box[2] = {64, (cuuint32_t)(together < 4 ? 1 : together)}, step[2] = {1, 1};
+    return encoder()(map, Elem<T>::FORMAT ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, const_cast<char*>(base), dims, strides, box, step,
+                     CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 template <int D, class T>
-cudaError_t by_rows(const HxCore& core, const AttendArgs& a, cudaStream_t s) {
-    static size_t allowed[2][64];
-    if (a.max_q * a.group <= 16) return launch<D, 1, T>(core, a, allowed[0], s);
-    return launch<D, 4, T>(core, a, allowed[1], s);
+cudaError_t launch(const HxCore& core, AttendArgs a, cudaStream_t s) {
+    static size_t allowed[64];
+    Maps maps{};
+    if (!encoder()) return cudaErrorNotSupported;
+    const int64_t width = (int64_t)a.n_kv_heads * D, rows = (int64_t)(a.n_pages - 1) * a.page_rows + a.page_tokens;
+    bool ok = encode<T>(&maps.k, a.k, width, rows, a.token_bytes, a.chunk) && encode<T>(&maps.v, a.v, width, rows, a.token_bytes, a.chunk);
+    if (a.tree) ok = ok && encode<T>(&maps.k_draft, a.k_draft, width, (int64_t)a.n * a.max_q, a.draft_row_bytes, a.chunk) &&
+                     encode<T>(&maps.v_draft, a.v_draft, width, (int64_t)a.n * a.max_q, a.draft_row_bytes, a.chunk);
+    if (!ok) return cudaErrorInvalidValue;
+    a.row_tiles = hx_ceil_div(a.max_q * a.group, GROUP_ROWS);
+    const int64_t items = (int64_t)a.n * a.row_tiles;
+    a.planned = items <= PLAN_ITEMS;
+    cudaError_t e = hx_opt_in_smem(hx_attend_kernel<D, T>, Shape<D>::SMEM, allowed, 0);
+    if (e != cudaSuccess) return e;
+    const int blocks = std::min(core.n_sm, MAX_BLOCKS);
+    e = hx_launch_dependent(hx_attend_kernel<D, T>, dim3(blocks), dim3(THREADS), Shape<D>::SMEM, s, a, maps);
+    if (e != cudaSuccess) return e;
+    ++*core.launches;
+    e = hx_launch_dependent(hx_attend_join_kernel<D, T>, dim3(blocks), dim3(JOIN_THREADS), 0, s, a);
+    if (e == cudaSuccess) ++*core.launches;
+    return e;
 }
 
 template <class T>
 cudaError_t by_dim(const HxCore& core, const AttendArgs& a, int dim, cudaStream_t s) {
     switch (dim) {
-        case 64: return by_rows<64, T>(core, a, s);
-        case 96: return by_rows<96, T>(core, a, s);
-        default: return by_rows<128, T>(core, a, s);
+        case 64: return launch<64, T>(core, a, s);
+        case 96: return launch<96, T>(core, a, s);
+        default: return launch<128, T>(core, a, s);
     }
 }
 
@@ -704,6 +1006,9 @@ const char* why_not_heads(const hx_kv_cache* c, int n_q_heads) {
     if (why) return why;
     if (c->dtype != HX_DTYPE_F16 && c->dtype != HX_DTYPE_BF16) return "attention takes F16 and BF16 caches";
     if (c->head_dim != 64 && c->head_dim != 96 && c->head_dim != 128) return "attention takes a head_dim of 64, 96 or 128";
+    const int64_t token = (int64_t)c->n_kv_heads * c->head_dim;
+    if (c->page_stride % token || c->n_pages * (c->page_stride / token) >= (1LL << 31))
+        return "attention takes pages that lie a whole number of tokens apart, less than 2^31 tokens in all";
     if (n_q_heads < 1 || n_q_heads % c->n_kv_heads || n_q_heads / c->n_kv_heads > 128)
         return "n_q_heads must be 1 to 128 times n_kv_heads";
     return nullptr;
@@ -731,7 +1036,8 @@ AttendArgs args_of(const HxCore& core, const hx_kv_cache* c, int layer, const hx
     AttendArgs a{};
     a.k = static_cast<const char*>(c->k) + layer * c->layer_stride * 2;
     a.v = static_cast<const char*>(c->v) + layer * c->layer_stride * 2;
-    a.page_bytes = c->page_stride * 2;
+    a.chunk = hx_power_in(c->page_tokens, BN);
+    a.page_rows = (int)(c->page_stride / ((int64_t)c->n_kv_heads * c->head_dim));
     a.token_bytes = c->n_kv_heads * c->head_dim * 2;
     a.page_tokens = c->page_tokens; a.n_pages = c->n_pages; a.max_seqs = c->max_seqs; a.max_pages = c->max_pages; a.n_kv_heads = c->n_kv_heads;
     a.table = c->table; a.len = c->len;
@@ -739,6 +1045,7 @@ AttendArgs args_of(const HxCore& core, const hx_kv_cache* c, int layer, const hx
     a.out = static_cast<char*>(io->out); a.o_row = io->out_row_stride; a.o_head = io->out_head_stride;
     a.lse = io->lse; a.n_rows = io->n_rows; a.group = io->n_q_heads / c->n_kv_heads;
     a.scale_log2 = io->scale * LOG2E;
+    a.out16 = reinterpret_cast<uintptr_t>(io->out) % 16 == 0 && io->out_row_stride % 8 == 0 && io->out_head_stride % 8 == 0;
     a.seqs = seqs; a.n = n;
     a.desc = static_cast<int4*>(io->work);
     a.part = reinterpret_cast<float*>(a.desc + MAX_BLOCKS);
@@ -766,7 +1073,7 @@ extern "C" {
 int hx_attend_work(const hx_kv_cache* cache, int n_q_heads, size_t* bytes) {
     const char* why = bytes ? why_not_heads(cache, n_q_heads) : "NULL buffer";
     if (why) return hx_fail(nullptr, HX_ERR_INVALID_ARG, why);
-    *bytes = MAX_BLOCKS * sizeof(int4) + part_bytes(cache->head_dim, 64);
+    *bytes = MAX_BLOCKS * sizeof(int4) + part_bytes(cache->head_dim);
     return HX_OK;
 }
 

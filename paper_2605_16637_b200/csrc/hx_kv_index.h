@@ -21,6 +21,10 @@ HX_HD int hx_page_at(const int32_t* row, int max_pages, int n_pages, int page_to
     return (p >= 0 && p < n_pages) ? p : -1;
 }
 
+// n rounded up to a multiple of the power of two `to`, as far as whole numbers go.
+HX_HD int hx_round_up(int n, int to) { return n > 0x7fffffff - to ? 0x7fffffff & ~(to - 1) : (n + to - 1) & ~(to - 1); }
+// The largest power of two that divides n, at most `most`.
+HX_HD int hx_power_in(int n, int most) { int p = 1; while (p < most && n % (2 * p) == 0) p *= 2; return p; }
 HX_HD int hx_ceil_div(int a, int b) { return a / b + (a % b != 0); }
 
 // Length of a sequence as the kernels take it: what the table row can hold at most, and no less than nothing.
@@ -29,16 +33,18 @@ HX_HD int hx_len_ok(int len, int max_pages, int page_tokens) {
 }
 
 // The positions that at least one query of a tile sees, as one axis without the gap between the first tokens and the
-// window: entry x is position x below n_sink and x + gap from there on; n entries.
+// window: entry x is position x below n_sink and x + gap from there on; n entries.  n_sink and gap are multiples of
+// `align`, so that stretches of that many entries are stretches of positions too; a few more are on the axis than are seen.
 struct HxAxis { int n_sink, gap, n; };
 
 // Queries at positions p_first .. p_last, each of which sees j <= p with j > p - window or j < sinks.
-HX_HD HxAxis hx_window_axis(int p_first, int p_last, int window, int sinks) {
+HX_HD HxAxis hx_window_axis(int p_first, int p_last, int window, int sinks, int align) {
     const int hi = p_last + 1;
     int lo = p_first - window + 1;                       // p_first >= 0, window >= 0: no overflow
     if (lo < 0) lo = 0;
-    int n_sink = sinks < lo ? sinks : lo;
-    if (n_sink > hi) n_sink = hi;
+    lo &= ~(align - 1);
+    int n_sink = sinks < lo ? hx_round_up(sinks, align) : lo;     // lo is a multiple: no further than lo
+    if (n_sink > hi) n_sink = hi & ~(align - 1);
     HxAxis a;
     a.n_sink = n_sink;
     a.gap = lo - n_sink;
@@ -52,6 +58,7 @@ HX_HD bool hx_window_sees(int p, int j, int window, int sinks) { return j <= p &
 // Whether every query of p_first .. p_last sees every entry of [xa, xb] (xb < a.n): no mask is needed there.
 HX_HD bool hx_window_full(const HxAxis& a, int xa, int xb, int p_first, int p_last, int window, int sinks) {
     if (xb >= a.n || hx_axis_pos(a, xb) > p_first) return false;
+    if (xa < a.n_sink && xb >= sinks && a.n_sink > sinks) return false;      // entries that only the alignment put there
     int x = xa > a.n_sink ? xa : a.n_sink;
     int px = x + a.gap;
     if (px < sinks) px = sinks;

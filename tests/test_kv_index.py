@@ -14,7 +14,9 @@ HARNESS = r"""
 extern "C" {
 int page_at(const int32_t* row, int mp, int np, int pt, int pos) { return hx_page_at(row, mp, np, pt, pos); }
 int len_ok(int len, int mp, int pt) { return hx_len_ok(len, mp, pt); }
-void axis(int a, int b, int w, int s, int* out) { HxAxis x = hx_window_axis(a, b, w, s); out[0] = x.n_sink; out[1] = x.gap; out[2] = x.n; }
+int round_up(int n, int to) { return hx_round_up(n, to); }
+int power_in(int n, int most) { return hx_power_in(n, most); }
+void axis(int a, int b, int w, int s, int al, int* out) { HxAxis x = hx_window_axis(a, b, w, s, al); out[0] = x.n_sink; out[1] = x.gap; out[2] = x.n; }
 int axis_pos(const int* x, int i) { HxAxis a; a.n_sink = x[0]; a.gap = x[1]; a.n = x[2]; return hx_axis_pos(a, i); }
 int sees(int p, int j, int w, int s) { return hx_window_sees(p, j, w, s); }
 int full(const int* x, int xa, int xb, int a, int b, int w, int s) { HxAxis y; y.n_sink = x[0]; y.gap = x[1]; y.n = x[2]; return hx_window_full(y, xa, xb, a, b, w, s); }
@@ -54,20 +56,20 @@ def test_lengths(lib):
     assert lib.len_ok(2147483647, 1 << 20, 1 << 20)                  # the product does not wrap
 
 
-def test_axis_holds_exactly_what_some_query_sees(lib):
+def test_axis_holds_what_some_query_sees(lib):
     rng = random.Random(5)
-    for _ in range(4000):
+    for _ in range(6000):
         a = rng.randrange(0, 60)
         b = a + rng.randrange(0, 20)
-        w, s = rng.choice((0, 1, 2, rng.randrange(1, 70))), rng.choice((0, 1, rng.randrange(0, 80)))
+        w, s, align = rng.choice((0, 1, 2, rng.randrange(1, 70))), rng.choice((0, 1, rng.randrange(0, 80))), rng.choice((1, 1, 4, 8, 16))
         x = (ctypes.c_int * 3)()
-        lib.axis(a, b, w, s, x)
+        lib.axis(a, b, w, s, align, x)
         pos = [lib.axis_pos(x, i) for i in range(x[2])]
         assert pos == sorted(set(pos)) and all(0 <= j <= b for j in pos)
+        assert x[0] % align == 0 and x[1] % align == 0               # stretches of `align` entries are stretches of positions
         seen = {j for p in range(a, b + 1) for j in range(p + 1) if lib.sees(p, j, w, s)}
-        assert seen <= set(pos)
-        for j in seen:                                               # the definition itself
-            assert any(j <= p and (j > p - w or j < s) for p in range(a, b + 1))
+        assert seen == {j for p in range(a, b + 1) for j in range(p + 1) if j > p - w or j < s}      # the definition itself
+        assert seen <= set(pos) and (align > 1 or w == 0 or seen == set(pos))
         for xa in range(0, max(1, x[2]), 8):
             xb = xa + 7
             if lib.full(x, xa, xb, a, b, w, s):
@@ -77,15 +79,21 @@ def test_axis_holds_exactly_what_some_query_sees(lib):
 def test_axis_at_the_ends_of_the_range(lib):
     big = 2147483647
     x = (ctypes.c_int * 3)()
-    lib.axis(0, big - 1, big, 0, x)
+    lib.axis(0, big - 1, big, 0, 1, x)
     assert list(x) == [0, 0, big]
-    lib.axis(big - 1, big - 1, 1, big, x)
+    lib.axis(big - 1, big - 1, 1, big, 1, x)
     assert list(x) == [big - 1, 0, big]
-    lib.axis(big - 1, big - 1, 16, 4, x)
+    lib.axis(big - 1, big - 1, 16, 4, 1, x)
     assert list(x) == [4, big - 16 - 4, 20]
-    lib.axis(5, 5, 0, 0, x)
+    lib.axis(big - 1, big - 1, 16, 4, 16, x)
+    assert list(x) == [16, big - 31 - 16, 16 + 31]
+    lib.axis(big - 1, big - 1, 16, big, 128, x)
+    assert list(x) == [big - 127, 0, big]
+    lib.axis(5, 5, 0, 0, 1, x)
     assert x[2] == 0
     assert lib.tiles(0, 64) == 1 and lib.tiles(64, 64) == 1 and lib.tiles(65, 64) == 2 and lib.tiles(big, 64) == 1 << 25
+    assert [lib.round_up(n, 16) for n in (0, 1, 16, 17, big - 16, big)] == [0, 16, 16, 32, big - 15, big - 15]
+    assert [lib.power_in(n, 64) for n in (1, 7, 24, 100, 16, 48, 64, 4096)] == [1, 1, 8, 4, 16, 16, 64, 64]
 
 
 def test_shares_cover_the_line_once(lib):
