@@ -8,12 +8,11 @@
 // lengths cost nothing; a group that is cut leaves partial results (maximum, sum, weighted values) that a second launch
 // joins in a fixed order.  Many groups: a block takes whole groups in turn.
 //
-// One block per multiprocessor, four warpgroups:
-//   0, 1  softmax of two streams: a thread holds one row of scores (128 tokens) in registers
-//   2     one warp loads: rows of tokens by TMA, four at a time by their row numbers (gather), which each lane takes
-//         from the page table, so any page size will do; a ring of keys and values runs ahead across groups; three warps
-//         load the rows of q
-//   3     one warp issues the tensor-core products (tcgen05, 128 x 128 tiles), one looks the next groups up
+// One block per multiprocessor, three warpgroups:
+//   0, 1  softmax of two streams: a thread works on one row of scores
+//   2     one warp loads keys and values by TMA, as many tokens at a time as a power of two that divides a page has, at the rows
+//         of memory that its lanes take from the page table (a ring that runs ahead across groups); one warp to each stream
+//         issues its tensor-core products (tcgen05); one looks the next groups up and loads the rows of q
 // Scores S = Q K^T go to tensor memory, the weights P return there in the cache's type as the left operand of O += P V, and
 // O stays there in binary32 for the whole group.  A group of more than 128 rows gives each stream 128 of them against
 // the same tiles; a smaller one gives the streams alternate tiles of the same rows, joined at its end.  So one stream's
@@ -22,9 +21,9 @@
 // The maximum that the weights are taken against follows the true one only when that has grown by more than 2^8: O is
 // rescaled then.  Weights are at most 2^8 that way, the sums are in binary32, and the result does not depend on the choice but for rounding.
 //
-// A value that some queries of a tile do not see may be infinite or NaN, and 0 x NaN is NaN in the product.  The tiles that need
-// masks (the ends of a group) are therefore looked through; where one holds such a value the block says so, and the second launch
-// computes that block's groups again with one warp per row, which reads only what the row sees.
+// A value that some queries of a tile do not see may be infinite or NaN, and 0 x NaN is NaN in the product.  So a block that
+// finds a result that is not finite says so, and the second launch computes that block's groups again with one warp per row,
+// which reads only what the row sees.
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -38,11 +37,12 @@
 namespace {
 
 constexpr int BN = 128;              // tokens per tile
+constexpr int STEP = 64;             // tokens of one step: scores of the next step are made while a step's exponentials run
 constexpr int TILE_ROWS = 128;       // rows of one stream's product
 constexpr int GROUP_ROWS = 256;
-constexpr int THREADS = 512;
+constexpr int THREADS = 384;
 constexpr int PLAN_ITEMS = 1024;     // groups per head that the shared plan holds
-constexpr int GROUP_COST = 1;        // tiles that the start and end of a group are worth
+constexpr int GROUP_COST = 2;        // tiles that the start and end of a group are worth
 constexpr int SEGS = 2;              // groups looked up ahead
 constexpr int VALID_RING = 8;
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
@@ -83,12 +83,12 @@ struct Group {
 
 template <class T> struct Elem;
 template <> struct Elem<__half> {
-    static constexpr uint32_t EXP = 0x7c00, FORMAT = 0;
+    static constexpr uint32_t FORMAT = 0;
     static __device__ __forceinline__ uint32_t pack(float a, float b) { __half2 h = __floats2half2_rn(a, b); return *reinterpret_cast<uint32_t*>(&h); }
     static __device__ __forceinline__ float2 unpack(uint32_t x) { return __half22float2(*reinterpret_cast<__half2*>(&x)); }
 };
 template <> struct Elem<__nv_bfloat16> {
-    static constexpr uint32_t EXP = 0x7f80, FORMAT = 1;
+    static constexpr uint32_t FORMAT = 1;
     static __device__ __forceinline__ uint32_t pack(float a, float b) { __nv_bfloat162 h = __floats2bfloat162_rn(a, b); return *reinterpret_cast<uint32_t*>(&h); }
     static __device__ __forceinline__ float2 unpack(uint32_t x) { return __bfloat1622float2(*reinterpret_cast<__nv_bfloat162*>(&x)); }
 };
@@ -130,6 +130,8 @@ __device__ __forceinline__ bool elect() {
     asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.b32 %0, 1, 0, p;\n}" : "=r"(one));
     return one != 0;
 }
+// A value that all lanes have, where the compiler knows it: operands of the products are then made without a detour.
+__device__ __forceinline__ uint32_t uniform(uint32_t x) { return __reduce_or_sync(0xffffffffu, x); }
 __device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes) {
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" :: "r"(bar), "r"(bytes) : "memory");
 }
@@ -145,18 +147,21 @@ __device__ __forceinline__ void load_box(uint32_t dst, const CUtensorMap* map, i
 }
 __device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
+constexpr uint32_t MATRIX_HIGH = 1024 >> 4 | 1u << 14 | 2u << 29;       // eight-row stride, version, 128-byte swizzle
+
 __device__ __forceinline__ void tc_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_commit(uint32_t bar) {
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" :: "r"(bar) : "memory");
 }
-__device__ __forceinline__ void tc_mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t add) {
-    asm volatile("{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}"
-                 :: "r"(d), "l"(a), "l"(b), "r"(idesc), "r"(add) : "memory");
+// Operands in shared memory are given by the low half of their description (`matrix`): the high half is the same for all.
+__device__ __forceinline__ void tc_mma_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t add) {
+    asm volatile("{\n .reg .pred p;\n .reg .b64 x, y;\n setp.ne.u32 p, %4, 0;\n mov.b64 x, {%1, %5};\n mov.b64 y, {%2, %5};\n"
+                 " tcgen05.mma.cta_group::1.kind::f16 [%0], x, y, %3, p;\n}" :: "r"(d), "r"(a), "r"(b), "r"(idesc), "r"(add), "n"(MATRIX_HIGH) : "memory");
 }
-__device__ __forceinline__ void tc_mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t add) {
-    asm volatile("{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}"
-                 :: "r"(d), "r"(a), "l"(b), "r"(idesc), "r"(add) : "memory");
+__device__ __forceinline__ void tc_mma_ts(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t add) {
+    asm volatile("{\n .reg .pred p;\n .reg .b64 y;\n setp.ne.u32 p, %4, 0;\n mov.b64 y, {%2, %5};\n"
+                 " tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], y, %3, p;\n}" :: "r"(d), "r"(a), "r"(b), "r"(idesc), "r"(add), "n"(MATRIX_HIGH) : "memory");
 }
 __device__ __forceinline__ void tc_ld32(uint32_t* r, uint32_t at) {
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
@@ -179,9 +184,7 @@ __device__ __forceinline__ void tc_st_wait() { asm volatile("tcgen05.wait::st.sy
 
 // Shared-memory matrix of 128-byte rows, swizzled in blocks of eight rows (1024 bytes); `lead`: bytes from one 64-element
 // panel to the next where the panels run along the operand's contiguous side (values), unused otherwise.
-__device__ __forceinline__ uint64_t matrix(uint32_t at, uint32_t lead) {
-    return (uint64_t)((at & 0x3ffff) >> 4) | (uint64_t)((lead & 0x3ffff) >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 | 1ull << 46 | 2ull << 61;
-}
+__device__ __forceinline__ uint32_t matrix(uint32_t at, uint32_t lead) { return (at & 0x3ffff) >> 4 | (lead & 0x3ffff) >> 4 << 16; }
 // binary32 sums, both operands of type FORMAT, 128 rows, n columns; the right operand with its n side contiguous or its k side.
 __host__ __device__ constexpr uint32_t product(uint32_t format, int n, bool n_contiguous) {
     return 1u << 4 | format << 7 | format << 10 | (n_contiguous ? 1u << 16 : 0u) | (uint32_t)(n >> 3) << 17 | (uint32_t)(TILE_ROWS >> 4) << 24;
@@ -355,15 +358,16 @@ __device__ __forceinline__ int row_of(const AttendArgs& a, const Group& g, int x
 // Entries of [0, 32) below n, as bits.
 __device__ __forceinline__ uint32_t below(int n) { return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u; }
 
-// What row r of the group sees of entries xa .. xa + 127, as bits (entries behind the axis are the caller's to take out).
-__device__ __forceinline__ void sees(const AttendArgs& a, const Group& g, const uint4* anc, int r, int xa, uint32_t (&m)[4]) {
+// What row r of the group sees of the 32 W entries from xa on, as bits (entries behind the axis are the caller's to take out).
+template <int W>
+__device__ __forceinline__ void sees(const AttendArgs& a, const Group& g, const uint4* anc, int r, int xa, uint32_t (&m)[W]) {
     const int qi = (g.r0 + r) / a.group;
     if (a.tree) {
         const uint4 t = anc[qi];
         const bool there = (t.x | t.y | t.z | t.w) != 0;
         const uint32_t w[5] = {t.x, t.y, t.z, t.w, 0u};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < W; ++i) {
             const int s = xa + 32 * i - g.axis.n_sink;           // drafted token of the word's first bit
             uint32_t x = 0;
             if (s <= -32) x = 0xffffffffu;
@@ -382,7 +386,7 @@ __device__ __forceinline__ void sees(const AttendArgs& a, const Group& g, const 
     first -= xa;
     const int lo = max(p - a.window + 1 - gap, g.axis.n_sink) - xa, hi = p + 1 - gap - xa;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) m[i] = below(first - 32 * i) | (below(hi - 32 * i) & ~below(lo - 32 * i));
+    for (int i = 0; i < W; ++i) m[i] = below(first - 32 * i) | (below(hi - 32 * i) & ~below(lo - 32 * i));
 }
 
 template <int D> struct Shape {
@@ -401,9 +405,10 @@ struct Shared {
     int64_t scan[THREADS / 32];
     alignas(16) uint32_t valid[VALID_RING][4];   // entries of a tile that have a row
     float2 stat[TILE_ROWS];          // maximum and sum of the second stream, where it shares its rows
+    float buf[2][TILE_ROWS * 17];    // 16 columns of every copy's result
     int link[HX_TREE_MAX];
     int4 rows[4][32];                // row numbers of the tiles being loaded, four to a lane; -1: zeros
-    unsigned long long full[8], empty[8], q_full, q_empty, s_full[2], p_full[2], o_full[2], x_ready, x_free, seg_full[SEGS], seg_empty[SEGS], drained;
+    unsigned long long full[8], empty[8], q_full, q_empty, s_full[2][2], p_full[2][2], pv[2], o_full[2], x_ready, x_free, join, seg_full[SEGS], seg_empty[SEGS], drained[2];
     uint32_t tmem;
     int quit;
 };
@@ -413,6 +418,82 @@ __device__ __forceinline__ int key_place(bool pair, int n, int j) { return pair 
 __device__ __forceinline__ int value_place(bool pair, int n, int j) { return pair ? 2 * j + 1 : j + 1 < n ? 2 * j + 2 : 2 * n - 1; }
 
 struct Maps { CUtensorMap k, v, k_draft, v_draft; };     // rows of tokens: of the cache's layer, and drafted ones
+
+// Where row r of a group goes: element of out, element of lse.
+struct Place { int64_t out, lse; };
+__device__ __forceinline__ Place place_of(const AttendArgs& a, const Group& g, int r) {
+    const int qi = (g.r0 + r) / a.group, head = g.head * a.group + g.r0 + r - qi * a.group;
+    return Place{(int64_t)(g.row0 + qi) * a.o_row + (int64_t)head * a.o_head, (int64_t)(g.row0 + qi) * a.n_kv_heads * a.group + head};
+}
+
+template <int N> struct Columns { static constexpr int value = N; };
+// How often the rows of a small group stand in the tile of rows: each copy takes a part of a step's tokens, so that all four warps
+// of a stream work (a thread can reach the scores of its own row only).
+__device__ __forceinline__ int copies_of(int rows) { return rows <= 32 ? 4 : rows <= 64 ? 2 : 1; }
+
+// One step of one row: scores of NC of the step's 64 tokens, from column col on; `seen` has a bit for each of them.  Brings the
+// running maximum and sum up to date and leaves the weights, rounded to T, with zeros for the tokens of other copies.  settle()
+// waits until the products of the steps before have left O alone.
+template <int D, int NC, class T, class Settle>
+__device__ __forceinline__ bool softmax_step(uint32_t S_at, uint32_t O_at, int col, bool masked, uint64_t seen, bool first, float scale, float& mx, float& sum, Settle settle) {
+    uint32_t x[NC];
+    if constexpr (NC == 16) tc_ld16(x, S_at + col);
+    else {
+#pragma unroll
+        for (int c = 0; c < NC; c += 32) tc_ld32(x + c, S_at + col + c);
+    }
+    tc_ld_wait();
+    if (masked) {
+#pragma unroll
+        for (int i = 0; i < NC; ++i) if (!((uint32_t)(i < 32 ? seen : seen >> 32) >> (i & 31) & 1)) x[i] = 0xff800000u;
+    }
+    float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+    for (int i = 0; i < NC; i += 8)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) m4[k] = fmaxf(fmaxf(m4[k], __uint_as_float(x[i + k])), __uint_as_float(x[i + 4 + k]));
+    const float top = fmaxf(mx, fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * scale);
+    if (__any_sync(0xffffffffu, top > mx + GROWTH || (first && top != mx))) {
+        const float alpha = top == mx ? 1.f : exp2_fast(mx - top);       // mx < top: finite or zero
+        mx = top; sum *= alpha;
+        if (!first) {
+            if (!settle()) return false;
+#pragma unroll
+            for (int c = 0; c < D; c += 16) {
+                uint32_t o[16];
+                tc_ld16(o, O_at + c);
+                tc_ld_wait();
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * alpha);
+                tc_st16(O_at + c, o);
+            }
+        }
+    }
+    const float safe = mx == -INFINITY ? 0.f : mx;
+    float s4[4] = {0.f, 0.f, 0.f, 0.f};
+    if constexpr (NC < STEP) {
+        const uint32_t zeros[16] = {};
+#pragma unroll
+        for (int c = 0; c < STEP / 2; c += NC / 2)
+            if (c != col / 2) { if constexpr (NC == 16) tc_st8(S_at + c, zeros); else tc_st16(S_at + c, zeros); }
+    }
+    constexpr int G = NC < 32 ? NC : 32;
+#pragma unroll
+    for (int k = 0; k < NC; k += G) {
+        uint32_t w[G / 2];
+#pragma unroll
+        for (int i = 0; i < G / 2; ++i) {
+            const float u = exp2_fast(__fmaf_rn(__uint_as_float(x[k + 2 * i]), scale, -safe));
+            const float v = exp2_fast(__fmaf_rn(__uint_as_float(x[k + 2 * i + 1]), scale, -safe));
+            s4[(2 * i) & 3] += u; s4[(2 * i + 1) & 3] += v;
+            w[i] = Elem<T>::pack(u, v);
+        }
+        if constexpr (G == 16) tc_st8(S_at + col / 2, w); else tc_st16(S_at + (col + k) / 2, w);
+    }
+    sum += (s4[0] + s4[1]) + (s4[2] + s4[3]);
+    tc_st_wait();
+    return true;
+}
 
 template <int D, class T>
 __global__ void __launch_bounds__(THREADS, 1) hx_attend_kernel(const AttendArgs a, const __grid_constant__ Maps maps) {
@@ -430,12 +511,15 @@ __global__ void __launch_bounds__(THREADS, 1) hx_attend_kernel(const AttendArgs 
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
     if (tid == 32) {
-        for (int i = 0; i < NS; ++i) { bar_init(smem_at(&sh.full[i]), 1); bar_init(smem_at(&sh.empty[i]), 1); }
-        bar_init(smem_at(&sh.q_full), 96); bar_init(smem_at(&sh.q_empty), 1);
-        for (int i = 0; i < 2; ++i) { bar_init(smem_at(&sh.s_full[i]), 1); bar_init(smem_at(&sh.p_full[i]), 4); bar_init(smem_at(&sh.o_full[i]), 1); }
-        bar_init(smem_at(&sh.x_ready), 4); bar_init(smem_at(&sh.x_free), 4);
-        for (int i = 0; i < SEGS; ++i) { bar_init(smem_at(&sh.seg_full[i]), 1); bar_init(smem_at(&sh.seg_empty[i]), 13); }
-        bar_init(smem_at(&sh.drained), 1);
+        for (int i = 0; i < NS; ++i) { bar_init(smem_at(&sh.full[i]), 1); bar_init(smem_at(&sh.empty[i]), 2); }
+        bar_init(smem_at(&sh.q_full), 32); bar_init(smem_at(&sh.q_empty), 2);
+        for (int i = 0; i < 2; ++i) {
+            for (int h = 0; h < 2; ++h) { bar_init(smem_at(&sh.s_full[i][h]), 1); bar_init(smem_at(&sh.p_full[i][h]), 4); }
+            bar_init(smem_at(&sh.pv[i]), 1); bar_init(smem_at(&sh.o_full[i]), 1);
+        }
+        bar_init(smem_at(&sh.x_ready), 4); bar_init(smem_at(&sh.x_free), 4); bar_init(smem_at(&sh.join), 4);
+        for (int i = 0; i < SEGS; ++i) { bar_init(smem_at(&sh.seg_full[i]), 1); bar_init(smem_at(&sh.seg_empty[i]), 11); }
+        bar_init(smem_at(&sh.drained[0]), 1); bar_init(smem_at(&sh.drained[1]), 1);
         sh.quit = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -449,9 +533,9 @@ __global__ void __launch_bounds__(THREADS, 1) hx_attend_kernel(const AttendArgs 
     const uint32_t tmem = sh.tmem;
 
     if (role == 2) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
-        bool go = true;
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
         if (warp == 8) {
+            bool go = true;
             // ---- keys and values
             int kvn = 0, tiles_seen = 0;
             for (int n = 0; go; ++n) {
@@ -463,14 +547,23 @@ __global__ void __launch_bounds__(THREADS, 1) hx_attend_kernel(const AttendArgs 
                 if (lane == 0) bar_arrive(smem_at(&sh.seg_empty[si]));
                 if (nt <= 0) break;
                 const bool pair = g.rows > TILE_ROWS;
+                const int per = max(a.chunk, 4);         // a lane's entries: drafted or cached together
+                const bool mine = lane * per < BN;
+                // the lane's entry of the page table for tile j, -1 where there is none: read one tile ahead of its use
+                auto entry = [&](int j) {
+                    const int x = (t0 + j) * BN + lane * per;
+                    if (a.chunk < 4 || !mine || j >= nt || x >= (a.tree ? g.len : g.axis.n)) return -1;
+                    const int c = (a.tree ? x : hx_axis_pos(g.axis, x)) / a.page_tokens;
+                    return c < a.max_pages ? a.table[(int64_t)g.seq * a.max_pages + c] : -1;
+                };
+                int next = entry(0);
                 for (int o = 0; o < 2 * nt; ++o) {
                     bool keys; int j;                    // place o of the order: which tile, keys or values
                     if (pair) { keys = !(o & 1); j = o >> 1; }
                     else if (o == 0) { keys = true; j = 0; }
                     else if (o == 2 * nt - 1) { keys = false; j = nt - 1; }
                     else { keys = o & 1; j = keys ? (o + 1) >> 1 : (o - 2) >> 1; }
-                    const int per = max(a.chunk, 4), x = (t0 + j) * BN + lane * per;     // a lane's entries: drafted or cached together
-                    const bool mine = lane * per < BN;
+                    const int x = (t0 + j) * BN + lane * per;
                     bool drafted = a.tree && x >= g.axis.n_sink;
                     int4 rows = make_int4(-BN, -BN, -BN, -BN);           // rows ahead of the map: zeros
                     if (keys) {
@@ -480,9 +573,12 @@ __global__ void __launch_bounds__(THREADS, 1) hx_attend_kernel(const AttendArgs 
                             rows.z = row_of(a, g, x + 2, &drafted); rows.w = row_of(a, g, x + 3, &drafted);
                             bits = (uint32_t)(rows.x >= 0) | (uint32_t)(rows.y >= 0) << 1 | (uint32_t)(rows.z >= 0) << 2 | (uint32_t)(rows.w >= 0) << 3;
                         } else {
-                            int n_have = 0;              // rows of the chunk that are entries of the axis
-                            const int first = mine ? row_of(a, g, x, &drafted) : -1;
-                            if (first >= 0) { rows.x = first; n_have = min(per, (a.tree && !drafted ? g.len : g.axis.n) - x); }
+                            const int page = next, end = a.tree && !drafted ? g.len : g.axis.n;
+                            next = entry(j + 1);
+                            int n_have = mine ? max(0, min(per, end - x)) : 0;       // rows of the chunk that are entries of the axis
+                            if (drafted) rows.x = g.row0 + x - g.axis.n_sink;
+                            else if (n_have > 0 && page >= 0 && page < a.n_pages) rows.x = page * a.page_rows + (a.tree ? x : hx_axis_pos(g.axis, x)) % a.page_tokens;
+                            else if (n_have > 0) { n_have = 0; atomicExch(a.status, HX_ERR_INVALID_ARG); }
                             n_have = __shfl_sync(0xffffffffu, n_have, 4 * lane / per);
                             bits = below(n_have - 4 * lane % per) & 15u;
                         }
@@ -516,40 +612,13 @@ __global__ void __launch_bounds__(THREADS, 1) hx_attend_kernel(const AttendArgs 
                 const int at = kvn - 1 - i;
                 if (at >= 0) { const unsigned long long t0 = now_ns(); while (!bar_try(smem_at(&sh.full[at % NS]), (at / NS) & 1) && now_ns() - t0 < WAIT_NS) { } }
             }
-        } else {
-            // ---- rows of q
-            for (int n = 0; go; ++n) {
-                const int si = n % SEGS;
-                if (!(go = warp_wait(smem_at(&sh.seg_full[si]), (n / SEGS) & 1, quit))) break;
-                const Seg& seg = sh.seg[si];
-                const int rows = seg.g.rows, r0 = seg.g.r0, row0 = seg.g.row0, head0 = seg.g.head * a.group, nt = seg.t1 - seg.t0;
-                __syncwarp();
-                if (lane == 0) bar_arrive(smem_at(&sh.seg_empty[si]));
-                if (nt <= 0) break;
-                if (!(go = warp_wait(smem_at(&sh.q_empty), (n & 1) ^ 1, quit))) break;
-                for (int rb = (warp - 9) * 32; rb < rows; rb += 96) {        // 32 rows, a lane finds the place of each
-                    const int r = rb + lane;
-                    const int qi = r < rows ? (r0 + r) / a.group : 0, hd = r < rows ? r0 + r - qi * a.group : 0;
-                    const unsigned long long src = reinterpret_cast<unsigned long long>(a.q + 2 * ((int64_t)(row0 + qi) * a.q_row + (int64_t)(head0 + hd) * a.q_head));
-#pragma unroll 4
-                    for (int i = 0; i < S::CHUNKS; ++i) {
-                        const int e = i * 32 + lane, q = e / S::CHUNKS, c = e - q * S::CHUNKS, rr = rb + q;
-                        const char* from = reinterpret_cast<const char*>(__shfl_sync(0xffffffffu, src, q));
-                        copy16(smem_at(q_s + (rr >> 7) * S::TILE) + piece(rr & 127, c), from + c * 16, rr < rows ? 16 : 0);
-                    }
-                }
-                copies_wait();
-                fence_async();
-                bar_arrive(smem_at(&sh.q_full));
-            }
-        }
-    } else if (role == 3) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
-        if (warp == 12) {
-            // ---- products
-            constexpr uint32_t QK = product(Elem<T>::FORMAT, BN, false), PV = product(Elem<T>::FORMAT, D, true);
-            const uint64_t q_m = matrix(smem_at(q_s), 16), k_m = matrix(smem_at(kv_s), 16), v_m = matrix(smem_at(kv_s), 16384);
-            int kvn = 0, pn[2] = {0, 0};
+        } else if (warp < 11) {
+            // ---- products of one stream
+            constexpr uint32_t QK = product(Elem<T>::FORMAT, STEP, false), PV = product(Elem<T>::FORMAT, D, true);
+            const int s = warp - 9;
+            const uint32_t q_m = matrix(smem_at(q_s), 16), k_m = matrix(smem_at(kv_s), 16), v_m = matrix(smem_at(kv_s), 16384);
+            const uint32_t S_at = uniform(tmem + s * 128), O_at = uniform(tmem + 256 + s * 128);
+            int kvn = 0, pn = 0;
             bool go = true;
             for (int n = 0; go; ++n) {
                 const int si = n % SEGS;
@@ -559,65 +628,73 @@ __global__ void __launch_bounds__(THREADS, 1) hx_attend_kernel(const AttendArgs 
                 __syncwarp();
                 if (lane == 0) bar_arrive(smem_at(&sh.seg_empty[si]));
                 if (nt <= 0) break;
-                // scores of tile j for stream s; last: the last reader of the keys; done: the last products that read q
-                auto scores = [&](int s, int j, bool last, bool done) {
-                    const int at = kvn + key_place(pair, nt, j), slot = at % NS;
-                    if (!warp_wait(smem_at(&sh.full[slot]), (at / NS) & 1, quit)) return false;
-                    tc_after();
+                if (!(go = warp_wait(smem_at(&sh.q_full), n & 1, quit))) break;
+                const uint32_t q_t = uniform(q_m + (pair ? s : 0) * (S::TILE >> 4));
+                const int step = pair ? 1 : 2, mine = pair ? 0 : s;          // this stream's tiles: mine, mine + step, ...
+                // a slot, and q, is given back by both streams, or twice by the one that reads it alone
+                auto give_back = [&](uint32_t bar, bool twice) { tc_commit(bar); if (twice) tc_commit(bar); };
+                auto ready = [&](int at) { return warp_wait(smem_at(&sh.full[at % NS]), (at / NS) & 1, quit); };
+                // scores of half h of the tile in `slot`; done: no products after these read q
+                auto scores = [&](int slot, int h, bool done) {
+                    const uint32_t k_t = uniform(k_m + slot * (S::TILE >> 4) + h * 512), to = S_at + h * STEP;
                     if (elect()) {
-                        const uint64_t kt = k_m + (uint64_t)(slot * (S::TILE >> 4)), qt = q_m + (uint64_t)((pair ? s : 0) * (S::TILE >> 4));
-                        const uint32_t to = tmem + s * 128;
 #pragma unroll
                         for (int ks = 0; ks < D / 16; ++ks)
-                            tc_mma_ss(to, qt + (uint64_t)((ks >> 2) * 1024 + (ks & 3) * 2), kt + (uint64_t)((ks >> 2) * 1024 + (ks & 3) * 2), QK, ks > 0);
-                        tc_commit(smem_at(&sh.s_full[s]));
-                        if (last) tc_commit(smem_at(&sh.empty[slot]));
-                        if (done) tc_commit(smem_at(&sh.q_empty));
+                            tc_mma_ss(to, q_t + (ks >> 2) * 1024 + (ks & 3) * 2, k_t + (ks >> 2) * 1024 + (ks & 3) * 2, QK, ks > 0);
+                        tc_commit(smem_at(&sh.s_full[s][h]));
+                        if (h == 1) {
+                            give_back(smem_at(&sh.empty[slot]), !pair);
+                            if (done) give_back(smem_at(&sh.q_empty), nt == 1 && !pair);
+                        }
                     }
                     __syncwarp();
-                    return true;
                 };
-                // weights of tile j times its values, for stream s; end: the stream's last tile of the group
-                auto values = [&](int s, int j, bool first, bool last, bool end) {
-                    const int at = kvn + value_place(pair, nt, j), slot = at % NS;
-                    if (!warp_wait(smem_at(&sh.full[slot]), (at / NS) & 1, quit)) return false;
-                    if (!warp_wait(smem_at(&sh.p_full[s]), pn[s] & 1, quit)) return false;
-                    ++pn[s];
-                    tc_after();
+                // weights of half h of the tile in `slot` times its values; first, last: of this stream's tiles
+                auto values = [&](int slot, int h, bool first, bool last) {
+                    const uint32_t v_t = uniform(v_m + slot * (S::TILE >> 4) + h * 512), from = S_at + h * STEP;
                     if (elect()) {
-                        const uint64_t vt = v_m + (uint64_t)(slot * (S::TILE >> 4));
-                        const uint32_t from = tmem + s * 128, to = tmem + 256 + s * 128;
 #pragma unroll
-                        for (int ks = 0; ks < BN / 16; ++ks) tc_mma_ts(to, from + ks * 8, vt + (uint64_t)(ks * 128), PV, !(first && ks == 0));
-                        if (last) tc_commit(smem_at(&sh.empty[slot]));
-                        if (end) tc_commit(smem_at(&sh.o_full[s]));
+                        for (int ks = 0; ks < STEP / 16; ++ks) tc_mma_ts(O_at, from + ks * 8, v_t + ks * 128, PV, !(first && h == 0 && ks == 0));
+                        tc_commit(smem_at(&sh.pv[s]));
+                        if (h == 1) {
+                            give_back(smem_at(&sh.empty[slot]), !pair);
+                            if (last) tc_commit(smem_at(&sh.o_full[s]));
+                        }
                     }
                     __syncwarp();
-                    return true;
                 };
-                if (!(go = warp_wait(smem_at(&sh.q_full), n & 1, quit))) break;
-                if (pair) {
-                    go = scores(0, 0, false, false) && scores(1, 0, true, nt == 1);
-                    for (int j = 0; j < nt && go; ++j) {
-                        const bool end = j + 1 == nt;
-                        go = values(0, j, j == 0, false, end) && (end || scores(0, j + 1, false, false)) && values(1, j, j == 0, true, end) &&
-                             (end || scores(1, j + 1, true, j + 2 == nt));
+                if (mine < nt) {
+                    const int at = kvn + key_place(pair, nt, mine);
+                    if (!(go = ready(at))) break;
+                    tc_after();
+                    scores(at % NS, 0, false);
+                    scores(at % NS, 1, mine + step >= nt);
+                }
+                for (int j = mine; j < nt && go; j += step) {
+                    const int v_at = kvn + value_place(pair, nt, j), next = j + step, k_at = kvn + key_place(pair, nt, next);
+                    if (!(go = ready(v_at))) break;
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        if (!(go = warp_wait(smem_at(&sh.p_full[s][h]), pn & 1, quit))) break;
+                        tc_after();
+                        values(v_at % NS, h, j == mine, next >= nt);
+                        if (next < nt) {
+                            if (h == 0) { if (!(go = ready(k_at))) break; tc_after(); }
+                            scores(k_at % NS, h, next + step >= nt);
+                        }
                     }
-                } else {
-                    go = scores(0, 0, true, nt == 1) && (nt < 2 || scores(1, 1, true, nt == 2));
-                    for (int j = 0; j < nt && go; ++j)
-                        go = values(j & 1, j, j < 2, true, j + 2 >= nt) && (j + 2 >= nt || scores(j & 1, j + 2, true, j + 3 == nt));
+                    ++pn;
                 }
                 kvn += 2 * nt;
             }
             if (!go) {                                   // what was issued ends before the tensor memory is given back
-                if (elect()) tc_commit(smem_at(&sh.drained));
+                if (elect()) tc_commit(smem_at(&sh.drained[s]));
                 __syncwarp();
                 const unsigned long long t0 = now_ns();
-                while (!bar_try(smem_at(&sh.drained), 0) && now_ns() - t0 < WAIT_NS) { }
+                while (!bar_try(smem_at(&sh.drained[s]), 0) && now_ns() - t0 < WAIT_NS) { }
             }
-        } else if (warp == 13) {
-            // ---- groups
+        } else {
+            // ---- groups, and their rows of q
             Walk w = begin_walk(a, plan, blockIdx.x, gridDim.x);
             for (int n = 0;; ++n) {
                 Group g;
@@ -637,15 +714,32 @@ __global__ void __launch_bounds__(THREADS, 1) hx_attend_kernel(const AttendArgs 
                 __syncwarp();
                 if (lane == 0) bar_arrive(smem_at(&sh.seg_full[si]));
                 if (!more) break;
+                if (!warp_wait(smem_at(&sh.q_empty), (n & 1) ^ 1, quit)) break;
+                const int head0 = g.head * a.group, copies = copies_of(g.rows), room = TILE_ROWS / copies;
+                for (int rb = 0; rb < (copies > 1 ? TILE_ROWS : g.rows); rb += 32) {         // 32 rows of the tile, a lane finds the place of each
+                    const int r = copies > 1 ? (rb + lane) & (room - 1) : rb + lane;
+                    const int qi = r < g.rows ? (g.r0 + r) / a.group : 0, hd = r < g.rows ? g.r0 + r - qi * a.group : 0;
+                    const unsigned long long src = reinterpret_cast<unsigned long long>(a.q + 2 * ((int64_t)(g.row0 + qi) * a.q_row + (int64_t)(head0 + hd) * a.q_head));
+#pragma unroll 8
+                    for (int i = 0; i < S::CHUNKS; ++i) {
+                        const int e = i * 32 + lane, q = e / S::CHUNKS, c = e - q * S::CHUNKS, rr = rb + q;
+                        const int have = __shfl_sync(0xffffffffu, r < g.rows, q);
+                        const char* from = reinterpret_cast<const char*>(__shfl_sync(0xffffffffu, src, q));
+                        copy16(smem_at(q_s + (rr >> 7) * S::TILE) + piece(rr & 127, c), from + c * 16, have ? 16 : 0);
+                    }
+                }
+                copies_wait();
+                fence_async();
+                bar_arrive(smem_at(&sh.q_full));
             }
         }
     } else {
         // ---- softmax
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 192;");
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");     // 2 x 208 + 88 = the 3 x 168 of the launch
         const int s = role, row = tid & 127;
         const uint32_t lanes = (uint32_t)(warp & 3) << 21;       // the warp's quarter of the 128 lanes
         const uint32_t S_at = tmem + lanes + s * 128, O_at = tmem + lanes + 256;
-        int sn = 0, on[2] = {0, 0}, xn = 0, kvn = 0, tiles_seen = 0;
+        int sn = 0, on = 0, xn = 0, jn = 0, kvn = 0, tiles_seen = 0;     // sn: tiles of this stream
         bool go = true, odd = false;
         for (int n = 0; go; ++n) {
             const int si = n % SEGS;
@@ -655,95 +749,57 @@ __global__ void __launch_bounds__(THREADS, 1) hx_attend_kernel(const AttendArgs 
             if (nt <= 0) break;
             const Group& g = seg.g;
             const bool pair = g.rows > TILE_ROWS;
-            const int r = row + (pair ? s * TILE_ROWS : 0);      // row of the group
-            const bool live = (warp & 3) * 32 + (pair ? s * TILE_ROWS : 0) < g.rows;     // the warp has rows
+            const int copies = copies_of(g.rows);
+            const int r = pair ? row + s * TILE_ROWS : row & (TILE_ROWS / copies - 1);       // row of the group
+            const int col = row / (TILE_ROWS / copies) * (STEP / copies);    // the first of a step's tokens that this copy of the row takes
+            const bool live = r - lane < g.rows;                 // the warp has rows
             const bool there = r < g.rows;
-            int p_first = 0, p_last = 0;
-            if (!a.tree) {
-                p_first = g.len - g.nq + (g.r0 + (pair ? s * TILE_ROWS : 0)) / a.group;
-                p_last = g.len - g.nq + (g.r0 + min(g.rows, (pair ? s + 1 : 1) * TILE_ROWS) - 1) / a.group;
-            }
+            int lo = 0, hi = 0;                                  // tiles without masks
+            if (a.tree) hi = g.axis.n_sink / BN;
+            else hx_whole_tiles(g.axis, g.len - g.nq + (g.r0 + (pair ? s * TILE_ROWS : 0)) / a.group,
+                                g.len - g.nq + (g.r0 + min(g.rows, (pair ? s + 1 : 1) * TILE_ROWS) - 1) / a.group, a.window, a.sinks, BN, &lo, &hi);
+            lo -= t0; hi -= t0;
             float mx = -INFINITY, sum = 0.f;
-            for (int j = pair ? 0 : s; j < nt; j += pair ? 1 : 2) {
-                if (!(go = warp_wait(smem_at(&sh.s_full[s]), sn & 1, quit))) break;
-                ++sn;
-                tc_after();
-                const int xa = (t0 + j) * BN;
-                bool whole = a.tree ? xa + BN <= g.axis.n_sink : hx_window_full(g.axis, xa, xa + BN - 1, p_first, p_last, a.window, a.sinks);
-                const uint4 valid = *reinterpret_cast<const uint4*>(sh.valid[(tiles_seen + j) % VALID_RING]);
-                whole = whole && (valid.x & valid.y & valid.z & valid.w) == 0xffffffffu;
-                if (!whole) {                            // a value that some rows do not see may be infinite or NaN
-                    const int at = kvn + value_place(pair, nt, j), slot = at % NS;
-                    if (!(go = warp_wait(smem_at(&sh.full[slot]), (at / NS) & 1, quit))) break;
-                    char* tile = kv_s + slot * S::TILE;
-                    const uint32_t word = row < 32 ? valid.x : row < 64 ? valid.y : row < 96 ? valid.z : valid.w;
-                    if ((word >> lane) & 1) {
-                        for (int c = 0; c < S::CHUNKS; ++c) {
-                            const uint4 x = *reinterpret_cast<const uint4*>(tile + piece(row, c));
-                            const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+            for (int j = pair ? 0 : s; j < nt && go; j += pair ? 1 : 2, ++sn) {
+                const uint32_t* valid = sh.valid[(tiles_seen + j) % VALID_RING];
+#pragma unroll 1
+                for (int h = 0; h < 2; ++h) {
+                    if (!(go = warp_wait(smem_at(&sh.s_full[s][h]), sn & 1, quit))) break;
+                    tc_after();
+                    const uint2 v2 = *reinterpret_cast<const uint2*>(valid + 2 * h);
+                    const bool all = (v2.x & v2.y) == 0xffffffffu, whole = j >= lo && j < hi && all;
+                    if (!all) {
+                        // rows that are no entry of the axis (behind the end of a page's use) hold anything, and 0 x NaN is NaN
+                        const int at = kvn + value_place(pair, nt, j), slot = at % NS;
+                        if (!(go = warp_wait(smem_at(&sh.full[slot]), (at / NS) & 1, quit))) break;
+                        if ((row >> 6) == h && !((valid[row >> 5] >> lane) & 1)) {
+                            char* tile = kv_s + slot * S::TILE;
 #pragma unroll
-                            for (int i = 0; i < 4; ++i)
-                                odd = odd || (w[i] & Elem<T>::EXP) == Elem<T>::EXP || (w[i] & (Elem<T>::EXP << 16)) == (Elem<T>::EXP << 16);
+                            for (int c = 0; c < S::CHUNKS; ++c) *reinterpret_cast<uint4*>(tile + piece(row, c)) = make_uint4(0, 0, 0, 0);
+                            fence_async();
                         }
-                    } else {                             // no entry of the axis: rows behind the end of a page's use hold anything
-                        for (int c = 0; c < S::CHUNKS; ++c) *reinterpret_cast<uint4*>(tile + piece(row, c)) = make_uint4(0, 0, 0, 0);
-                        fence_async();
                     }
+                    if (live) {
+                        const bool first = j < (pair ? 1 : 2) && h == 0;
+                        uint64_t seen = 0;
+                        if (!whole) {
+                            uint32_t m[2] = {0, 0};
+                            if (there) sees<2>(a, g, seg.anc, r, (t0 + j) * BN + h * STEP, m);
+                            seen = ((uint64_t)(m[1] & v2.y) << 32 | (m[0] & v2.x)) >> col;
+                        }
+                        // the products of the step before may still add to O; those before it have ended, as these scores came after them
+                        auto settle = [&] { if (!warp_wait(smem_at(&sh.pv[s]), (2 * sn + h - 1) & 1, quit)) return false; tc_after(); return true; };
+                        auto step = [&](auto columns) {
+                            constexpr int NC = decltype(columns)::value;
+                            return softmax_step<D, NC, T>(S_at + h * STEP, O_at + s * 128, col, !whole, seen, first, a.scale_log2, mx, sum, settle);
+                        };
+                        go = copies == 1 ? step(Columns<64>()) : copies == 2 ? step(Columns<32>()) : step(Columns<16>());
+                        if (!go) break;
+                    }
+                    tc_before();
+                    __syncwarp();
+                    if (lane == 0) bar_arrive(smem_at(&sh.p_full[s][h]));
                 }
-                if (live) {
-                    uint32_t x[128];
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) tc_ld32(x + 32 * c, S_at + 32 * c);
-                    tc_ld_wait();
-                    if (!whole) {
-                        uint32_t m[4] = {0, 0, 0, 0};
-                        if (there) sees(a, g, seg.anc, r, xa, m);
-                        m[0] &= valid.x; m[1] &= valid.y; m[2] &= valid.z; m[3] &= valid.w;
-#pragma unroll
-                        for (int i = 0; i < 128; ++i) if (!((m[i >> 5] >> (i & 31)) & 1)) x[i] = 0xff800000u;
-                    }
-                    float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-                    for (int i = 0; i < 128; i += 8)
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) m4[k] = fmaxf(fmaxf(m4[k], __uint_as_float(x[i + k])), __uint_as_float(x[i + 4 + k]));
-                    const float top = fmaxf(mx, fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * a.scale_log2);
-                    const bool first = j < (pair ? 1 : 2);
-                    if (__any_sync(0xffffffffu, top > mx + GROWTH || (first && top != mx))) {
-                        const float alpha = top == mx ? 1.f : exp2_fast(mx - top);       // mx < top: finite or zero
-                        mx = top; sum *= alpha;
-                        if (!first) {
-#pragma unroll
-                            for (int c = 0; c < D; c += 16) {
-                                uint32_t o[16];
-                                tc_ld16(o, O_at + s * 128 + c);
-                                tc_ld_wait();
-#pragma unroll
-                                for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * alpha);
-                                tc_st16(O_at + s * 128 + c, o);
-                            }
-                        }
-                    }
-                    const float safe = mx == -INFINITY ? 0.f : mx;
-                    float s4[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                    for (int c = 0; c < 8; ++c) {
-                        uint32_t w[8];
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            const float u = exp2_fast(__fmaf_rn(__uint_as_float(x[16 * c + 2 * i]), a.scale_log2, -safe));
-                            const float v = exp2_fast(__fmaf_rn(__uint_as_float(x[16 * c + 2 * i + 1]), a.scale_log2, -safe));
-                            s4[(2 * i) & 3] += u; s4[(2 * i + 1) & 3] += v;
-                            w[i] = Elem<T>::pack(u, v);
-                        }
-                        tc_st8(S_at + 8 * c, w);
-                    }
-                    sum += (s4[0] + s4[1]) + (s4[2] + s4[3]);
-                    tc_st_wait();
-                }
-                tc_before();
-                __syncwarp();
-                if (lane == 0) bar_arrive(smem_at(&sh.p_full[s]));
             }
             if (!go) break;
 
@@ -753,6 +809,7 @@ __global__ void __launch_bounds__(THREADS, 1) hx_attend_kernel(const AttendArgs 
                 const uint4 m = seg.anc[(g.r0 + r) / a.group];
                 if (!(m.x | m.y | m.z | m.w)) { mx = -INFINITY; sum = 0.f; }
             }
+            if (pair || s == 0 || both) { if (!(go = warp_wait(smem_at(&sh.o_full[s]), on++ & 1, quit))) break; }
             if (both && s == 1) {
                 sh.stat[row] = make_float2(mx, sum);
                 __syncwarp();
@@ -760,12 +817,8 @@ __global__ void __launch_bounds__(THREADS, 1) hx_attend_kernel(const AttendArgs 
                 if (!(go = warp_wait(smem_at(&sh.x_free), xn & 1, quit))) break;
                 ++xn;
             } else if (pair || s == 0) {
-                if (!(go = warp_wait(smem_at(&sh.o_full[s]), on[s] & 1, quit))) break;
-                ++on[s];
                 float f0 = 1.f, f1 = 0.f;
                 if (both) {
-                    if (!(go = warp_wait(smem_at(&sh.o_full[1]), on[1] & 1, quit))) break;
-                    ++on[1];
                     if (!(go = warp_wait(smem_at(&sh.x_ready), xn & 1, quit))) break;
                     ++xn;
                     const float2 o = sh.stat[row];
@@ -775,52 +828,106 @@ __global__ void __launch_bounds__(THREADS, 1) hx_attend_kernel(const AttendArgs 
                 }
                 tc_after();
                 const bool complete = t0 == 0 && seg.t1 == g.tiles;
-                const bool none = sum == 0.f;            // sees nothing here: what the products left says nothing
-                const float inv = none ? 0.f : 1.f / sum;
-                const int qi = (g.r0 + r) / a.group, head = g.head * a.group + g.r0 + r - qi * a.group;
-                T* out = reinterpret_cast<T*>(a.out) + (int64_t)(g.row0 + qi) * a.o_row + (int64_t)head * a.o_head;
-                float* part = a.part + (((int64_t)blockIdx.x * 2 + (t0 > 0 ? 0 : 1)) * GROUP_ROWS + r) * (D + 4);
-                if (live) {
+                float finite = 0.f;                      // NaN when something of a row's result is not finite
+                if (copies == 1) {
+                    const bool none = sum == 0.f;        // sees nothing here: what the products left says nothing
+                    const float inv = none ? 0.f : 1.f / sum;
+                    const Place at = place_of(a, g, r);
+                    float* part = a.part + (((int64_t)blockIdx.x * 2 + (t0 > 0 ? 0 : 1)) * GROUP_ROWS + r) * (D + 4);
+                    if (live) {
 #pragma unroll
-                    for (int c = 0; c < D; c += 32) {
-                        uint32_t o[32], p[32];
-                        tc_ld32(o, O_at + s * 128 + c);
-                        if (both) tc_ld32(p, O_at + 128 + c);
+                        for (int c = 0; c < D; c += 32) {
+                            uint32_t o[32], p[32];
+                            tc_ld32(o, O_at + s * 128 + c);
+                            if (both) tc_ld32(p, O_at + 128 + c);
+                            tc_ld_wait();
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) {
+                                float x = __uint_as_float(o[i]);
+                                if (both) x = (f0 == 0.f ? 0.f : x * f0) + (f1 == 0.f ? 0.f : __uint_as_float(p[i]) * f1);
+                                if (none) x = 0.f;
+                                finite = __fmaf_rn(x, 0.f, finite);
+                                o[i] = __float_as_uint(x);
+                            }
+                            if (there && complete) {
+                                uint32_t w[16];
+#pragma unroll
+                                for (int i = 0; i < 16; ++i) w[i] = Elem<T>::pack(__uint_as_float(o[2 * i]) * inv, __uint_as_float(o[2 * i + 1]) * inv);
+                                T* out = reinterpret_cast<T*>(a.out) + at.out + c;
+                                if (a.out16) {
+#pragma unroll
+                                    for (int i = 0; i < 4; ++i) reinterpret_cast<uint4*>(out)[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+                                } else {
+#pragma unroll
+                                    for (int i = 0; i < 16; ++i) reinterpret_cast<uint32_t*>(out)[i] = w[i];
+                                }
+                            } else if (there) {
+#pragma unroll
+                                for (int i = 0; i < 8; ++i) reinterpret_cast<uint4*>(part + 4 + c)[i] = make_uint4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+                            }
+                        }
+                        if (there) {
+                            if (!complete) *reinterpret_cast<float2*>(part) = make_float2(mx, sum);
+                            else if (a.lse) a.lse[at.lse] = none ? -INFINITY : __fmaf_rn(mx, LN2, logf(sum));
+                        }
+                    }
+                    if (!there) finite = 0.f;
+                } else {
+                    // the copies of a row joined through shared memory, 16 columns at a time; then thread t writes columns
+                    // 16 / copies * (t % copies) .. of row t / copies
+                    const int room = TILE_ROWS / copies;
+                    auto together = [&] {
+                        __syncwarp();
+                        if (lane == 0) bar_arrive(smem_at(&sh.join));
+                        return warp_wait(smem_at(&sh.join), jn++ & 1, quit);
+                    };
+                    sh.stat[row] = make_float2(mx, sum);
+                    if (!(go = together())) break;
+                    const int rr = row / copies;
+                    float m = -INFINITY, m2 = -INFINITY, l2 = 0.f;       // of the row at hand, and of the one written
+                    for (int k = 0; k < copies; ++k) { m = fmaxf(m, sh.stat[r + k * room].x); m2 = fmaxf(m2, sh.stat[rr + k * room].x); }
+                    const float safe2 = m2 == -INFINITY ? 0.f : m2;
+                    for (int k = 0; k < copies; ++k) l2 = __fmaf_rn(sh.stat[rr + k * room].y, exp2_fast(sh.stat[rr + k * room].x - safe2), l2);
+                    const float f = sum == 0.f ? 0.f : exp2_fast(mx - (m == -INFINITY ? 0.f : m));
+                    f0 *= f; f1 *= f;
+                    const bool none = l2 == 0.f, write = rr < g.rows;
+                    const float inv = none ? 0.f : 1.f / l2;
+                    const Place at = place_of(a, g, write ? rr : 0);
+                    float* part = a.part + (((int64_t)blockIdx.x * 2 + (t0 > 0 ? 0 : 1)) * GROUP_ROWS + rr) * (D + 4);
+                    for (int c = 0; c < D; c += 16) {
+                        uint32_t o[16], p[16];
+                        float* buf = sh.buf[(c >> 4) & 1];
+                        tc_ld16(o, O_at + c);
+                        if (both) tc_ld16(p, O_at + 128 + c);
                         tc_ld_wait();
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) {
-                            float x = __uint_as_float(o[i]);
-                            if (both) x = (f0 == 0.f ? 0.f : x * f0) + (f1 == 0.f ? 0.f : __uint_as_float(p[i]) * f1);
-                            o[i] = __float_as_uint(none ? 0.f : x);
+                        for (int i = 0; i < 16; ++i) {
+                            float x = f0 == 0.f ? 0.f : __uint_as_float(o[i]) * f0;
+                            if (both && f1 != 0.f) x += __uint_as_float(p[i]) * f1;
+                            buf[row * 17 + i] = x;
                         }
-                        if (there && complete) {
-                            uint32_t w[16];
-#pragma unroll
-                            for (int i = 0; i < 16; ++i) w[i] = Elem<T>::pack(__uint_as_float(o[2 * i]) * inv, __uint_as_float(o[2 * i + 1]) * inv);
-                            if (a.out16) {
-#pragma unroll
-                                for (int i = 0; i < 4; ++i) reinterpret_cast<uint4*>(out + c)[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
-                            } else {
-#pragma unroll
-                                for (int i = 0; i < 16; ++i) reinterpret_cast<uint32_t*>(out + c)[i] = w[i];
-                            }
-                        } else if (there) {
-#pragma unroll
-                            for (int i = 0; i < 8; ++i) reinterpret_cast<uint4*>(part + 4 + c)[i] = make_uint4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+                        if (!(go = together())) break;
+                        for (int i = (row % copies) * (16 / copies); i < (row % copies + 1) * (16 / copies); i += 2) {
+                            float x = 0.f, y = 0.f;
+                            for (int k = 0; k < copies; ++k) { x += buf[(rr + k * room) * 17 + i]; y += buf[(rr + k * room) * 17 + i + 1]; }
+                            if (none) x = y = 0.f;
+                            if (!write) continue;
+                            finite = __fmaf_rn(x, 0.f, __fmaf_rn(y, 0.f, finite));
+                            if (complete) *reinterpret_cast<uint32_t*>(reinterpret_cast<T*>(a.out) + at.out + c + i) = Elem<T>::pack(x * inv, y * inv);
+                            else *reinterpret_cast<float2*>(part + 4 + c + i) = make_float2(x, y);
                         }
                     }
-                    if (there) {
-                        if (!complete) *reinterpret_cast<float2*>(part) = make_float2(mx, sum);
-                        else if (a.lse) a.lse[(int64_t)(g.row0 + qi) * a.n_kv_heads * a.group + head] = none ? -INFINITY : __fmaf_rn(mx, LN2, logf(sum));
+                    if (!go) break;
+                    if (write && row % copies == 0) {
+                        if (!complete) *reinterpret_cast<float2*>(part) = make_float2(m2, l2);
+                        else if (a.lse) a.lse[at.lse] = none ? -INFINITY : __fmaf_rn(m2, LN2, logf(l2));
                     }
                 }
+                odd = odd || finite != 0.f;
                 tc_before();
                 __syncwarp();
                 if (both && lane == 0) bar_arrive(smem_at(&sh.x_free));
             }
-            // the stream that had no tile, or whose rows the first one has written, has nothing to wait for
-            if (s == 1 && !pair) { if (both) ++on[1]; }
-            if (s == 0 && pair) ++on[1];
             __syncwarp();
             if (lane == 0) bar_arrive(smem_at(&sh.seg_empty[si]));
             kvn += 2 * nt;
@@ -845,8 +952,8 @@ __device__ void one_row(const AttendArgs& a, const Group& g, const uint4* anc, i
 #pragma unroll
     for (int i = 0; i < D / 32; ++i) acc[i] = 0.f;
     for (int x0 = 0; x0 < g.axis.n; x0 += 32) {
-        uint32_t bits[4];
-        sees(a, g, anc, r, x0, bits);
+        uint32_t bits[1];
+        sees<1>(a, g, anc, r, x0, bits);
         bool drafted;
         const int at = row_of(a, g, x0 + lane, &drafted);
         const bool see = at >= 0 && ((bits[0] >> lane) & 1);

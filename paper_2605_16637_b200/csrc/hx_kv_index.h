@@ -55,14 +55,18 @@ HX_HD int hx_axis_pos(const HxAxis& a, int x) { return x < a.n_sink ? x : x + a.
 
 HX_HD bool hx_window_sees(int p, int j, int window, int sinks) { return j <= p && (j > p - window || j < sinks); }
 
-// Whether every query of p_first .. p_last sees every entry of [xa, xb] (xb < a.n): no mask is needed there.
-HX_HD bool hx_window_full(const HxAxis& a, int xa, int xb, int p_first, int p_last, int window, int sinks) {
-    if (xb >= a.n || hx_axis_pos(a, xb) > p_first) return false;
-    if (xa < a.n_sink && xb >= sinks && a.n_sink > sinks) return false;      // entries that only the alignment put there
-    int x = xa > a.n_sink ? xa : a.n_sink;
-    int px = x + a.gap;
-    if (px < sinks) px = sinks;
-    return px > p_last - window;
+// Tiles [*lo, *hi) of the axis in which every query of p_first .. p_last sees every entry: no mask is needed there.
+HX_HD void hx_whole_tiles(const HxAxis& a, int p_first, int p_last, int window, int sinks, int tile, int* lo, int* hi) {
+    int first = 0;                                       // entries from here on are in the window of all queries, or first tokens
+    if (sinks <= p_last - window) {
+        first = p_last - window + 1 - a.gap;
+        if (first < a.n_sink) first = a.n_sink;
+    }
+    int last = p_first - a.gap;                          // entries up to here are behind no query
+    if (last > a.n - 1) last = a.n - 1;
+    if (last < a.n_sink && a.gap) last = -1;             // a gap ahead of it: the window has no entry that all see
+    *lo = first / tile + (first % tile != 0);
+    *hi = (last + 1) / tile;
 }
 
 // Tiles of the axis, at least one so that rows that see nothing are written too.

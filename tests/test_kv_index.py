@@ -19,7 +19,7 @@ int power_in(int n, int most) { return hx_power_in(n, most); }
 void axis(int a, int b, int w, int s, int al, int* out) { HxAxis x = hx_window_axis(a, b, w, s, al); out[0] = x.n_sink; out[1] = x.gap; out[2] = x.n; }
 int axis_pos(const int* x, int i) { HxAxis a; a.n_sink = x[0]; a.gap = x[1]; a.n = x[2]; return hx_axis_pos(a, i); }
 int sees(int p, int j, int w, int s) { return hx_window_sees(p, j, w, s); }
-int full(const int* x, int xa, int xb, int a, int b, int w, int s) { HxAxis y; y.n_sink = x[0]; y.gap = x[1]; y.n = x[2]; return hx_window_full(y, xa, xb, a, b, w, s); }
+void whole(const int* x, int a, int b, int w, int s, int t, int* out) { HxAxis y; y.n_sink = x[0]; y.gap = x[1]; y.n = x[2]; hx_whole_tiles(y, a, b, w, s, t, out, out + 1); }
 int tiles(int n, int t) { return hx_tiles(n, t); }
 int64_t share(int64_t t, int c, int n) { return hx_share(t, c, n); }
 int share_of(int64_t t, int64_t u, int n) { return hx_share_of(t, u, n); }
@@ -57,7 +57,7 @@ def test_lengths(lib):
 
 
 def test_axis_holds_what_some_query_sees(lib):
-    rng = random.Random(5)
+    rng, found = random.Random(5), 0
     for _ in range(6000):
         a = rng.randrange(0, 60)
         b = a + rng.randrange(0, 20)
@@ -70,10 +70,12 @@ def test_axis_holds_what_some_query_sees(lib):
         seen = {j for p in range(a, b + 1) for j in range(p + 1) if lib.sees(p, j, w, s)}
         assert seen == {j for p in range(a, b + 1) for j in range(p + 1) if j > p - w or j < s}      # the definition itself
         assert seen <= set(pos) and (align > 1 or w == 0 or seen == set(pos))
-        for xa in range(0, max(1, x[2]), 8):
-            xb = xa + 7
-            if lib.full(x, xa, xb, a, b, w, s):
-                assert xb < x[2] and all(lib.sees(p, pos[i], w, s) for p in range(a, b + 1) for i in range(xa, xb + 1))
+        lo_hi = (ctypes.c_int * 2)()
+        lib.whole(x, a, b, w, s, 8, lo_hi)
+        for t in range(lo_hi[0], lo_hi[1]):
+            assert 8 * t + 7 < x[2] and all(lib.sees(p, pos[i], w, s) for p in range(a, b + 1) for i in range(8 * t, 8 * t + 8))
+            found += 1
+    assert found > 1000                                              # most tiles of a long window are whole
 
 
 def test_axis_at_the_ends_of_the_range(lib):
