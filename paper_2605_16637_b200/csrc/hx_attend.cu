@@ -2,21 +2,23 @@
 //
 // Work is a list of groups: up to 256 rows of the queries of one sequence that share a KV head (row r is query r / G, head
 // r % G of the G query heads), against the tokens that any of them sees.  The tokens form one axis without gaps (first tokens,
-// then window; or cached tokens, then drafted ones), cut into tiles of 128.
+// then window; or cached tokens, then drafted ones), cut into steps of 64.
 //
-// Few groups: the tiles of all groups form one line that is cut into equal shares, one per multiprocessor, so that ragged
+// Few groups: the steps of all groups form one line that is cut into equal shares, one per multiprocessor, so that ragged
 // lengths cost nothing; a group that is cut leaves partial results (maximum, sum, weighted values) that a second launch
 // joins in a fixed order.  Many groups: a block takes whole groups in turn.
 //
-// One block per multiprocessor, three warpgroups:
+// One block per multiprocessor, four warpgroups:
 //   0, 1  softmax of two streams: a thread works on one row of scores
-//   2     one warp loads keys and values by TMA, as many tokens at a time as a power of two that divides a page has, at the rows
-//         of memory that its lanes take from the page table (a ring that runs ahead across groups); one warp to each stream
-//         issues its tensor-core products (tcgen05); one looks the next groups up and loads the rows of q
+//   2     one warp to each stream issues its tensor-core products (tcgen05); one looks the next groups up and loads the rows of q
+//   3     four warps load keys and values by TMA, in turn: as many tokens at a time as a power of two that divides a page has, at the
+//         rows of memory that the lanes take from the page table (a ring that runs ahead across groups; one warp alone spends some
+//         75 cycles on each copy that it issues, which is more than the copies take)
 // Scores S = Q K^T go to tensor memory, the weights P return there in the cache's type as the left operand of O += P V, and
 // O stays there in binary32 for the whole group.  A group of more than 128 rows gives each stream 128 of them against
-// the same tiles; a smaller one gives the streams alternate tiles of the same rows, joined at its end.  So one stream's
-// products run while the other's exponentials do.
+// the same tokens; smaller ones are taken two KV heads at a time, one to a stream (a last head alone gives the streams alternate
+// steps, joined at its end).  A stream has two buffers for scores, so that those of a step are made while the exponentials of the
+// one before it run.
 //
 // The maximum that the weights are taken against follows the true one only when that has grown by more than 2^8: O is
 // rescaled then.  Weights are at most 2^8 that way, the sums are in binary32, and the result does not depend on the choice but for rounding.
@@ -36,15 +38,17 @@
 
 namespace {
 
-constexpr int BN = 128;              // tokens per tile
-constexpr int STEP = 64;             // tokens of one step: scores of the next step are made while a step's exponentials run
+constexpr int STEP = 64;             // tokens of a step
 constexpr int TILE_ROWS = 128;       // rows of one stream's product
 constexpr int GROUP_ROWS = 256;
-constexpr int THREADS = 384;
+constexpr int THREADS = 512;
+constexpr int LOADERS = 4;           // warps that load keys and values
 constexpr int PLAN_ITEMS = 1024;     // groups per head that the shared plan holds
-constexpr int GROUP_COST = 2;        // tiles that the start and end of a group are worth
+// Units of the line that is cut into shares: what a step costs both streams, what it costs when they take alternate ones, and what
+// the start and end of a group cost (measured: some 2,300, 1,500 and 7,000 cycles).
+constexpr int BOTH_COST = 3, ALTERNATE_COST = 2, GROUP_COST = 8;
 constexpr int SEGS = 2;              // groups looked up ahead
-constexpr int VALID_RING = 8;
+constexpr int VALID_RING = 16;
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 constexpr float GROWTH = 8.f;        // powers of two that the maximum may grow before O is rescaled
 constexpr unsigned long long WAIT_NS = 2000000000ull;    // a wait that lasts this long ends the kernel with HX_ERR_TIMEOUT
@@ -67,7 +71,7 @@ struct AttendArgs {
     int n, max_q, row_tiles;         // groups of a sequence and head: ceil(max_q * G / 256)
     int window, sinks;
     const char *k_draft, *v_draft; int64_t draft_row_bytes;
-    int tree, planned, out16;        // planned: shares of the line of tiles; else whole groups in turn; out16: 16-byte stores
+    int tree, planned, out16;        // planned: shares of the line of steps; else whole groups in turn; out16: 16-byte stores
     // partial results
     float* part; int4* desc;
     int* status;
@@ -75,7 +79,7 @@ struct AttendArgs {
 
 // One group: what the loads and the products need of it.
 struct Group {
-    int item, head, tiles;
+    int item, head, heads, steps;    // heads: KV heads that are taken together, one to a stream
     int seq, row0, nq, len;          // slot of the cache, first row of q, queries, tokens
     int r0, rows;                    // its first row, its rows (at most 256)
     HxAxis axis;                     // tree: n_sink = cached tokens up to a multiple of the chunk, n = those and the drafted ones
@@ -208,27 +212,33 @@ __device__ __forceinline__ bool request(const AttendArgs& a, int b, int* seq, in
 
 __device__ __forceinline__ Group group_of(const AttendArgs& a, int item, int head, bool report = false) {
     Group g;
-    g.item = item; g.head = head; g.tiles = 0;
+    g.item = item; g.head = head; g.steps = 0;
     const int b = item / a.row_tiles;
     g.r0 = (item - b * a.row_tiles) * GROUP_ROWS;
     if (!request(a, b, &g.seq, &g.row0, &g.nq, &g.len) && report && g.r0 == 0 && head == 0) atomicExch(a.status, HX_ERR_INVALID_ARG);
     g.rows = min(GROUP_ROWS, g.nq * a.group - g.r0);
+    g.heads = g.rows <= TILE_ROWS && head + 1 < a.n_kv_heads ? 2 : 1;
     g.axis.n_sink = g.axis.gap = g.axis.n = 0;
     if (g.rows <= 0) { g.rows = 0; return g; }
     if (a.tree) { g.axis.n_sink = hx_round_up(g.len, max(a.chunk, 4)); g.axis.n = g.axis.n_sink + g.nq; }
     else g.axis = hx_window_axis(g.len - g.nq + g.r0 / a.group, g.len - g.nq + (g.r0 + g.rows - 1) / a.group, a.window, a.sinks, a.chunk);
-    g.tiles = hx_tiles(g.axis.n, BN);
+    g.steps = hx_tiles(g.axis.n, STEP);
     return g;
 }
 
-// The line of tiles: prefix[i] = units before item i, per head (a group counts its tiles and GROUP_COST).
+// Steps over the KV heads of an item: of its groups, or pairs of groups.
+__device__ __forceinline__ int head_steps(const AttendArgs& a, int rows) { return rows > TILE_ROWS ? a.n_kv_heads : (a.n_kv_heads + 1) / 2; }
+
+// The line of steps: prefix[i] = units before item i.
+__device__ __forceinline__ int step_cost(const AttendArgs& a, int rows) { return rows > TILE_ROWS || a.n_kv_heads > 1 ? BOTH_COST : ALTERNATE_COST; }
 struct Plan { int64_t total; int shares; };
 __device__ Plan make_plan(const AttendArgs& a, int64_t* prefix, int64_t* scan, int n_blocks, bool report) {
     const int tid = threadIdx.x, nt = blockDim.x, lane = tid & 31, warp = tid >> 5, items = a.n * a.row_tiles;
     const int per = hx_ceil_div(items, nt), i0 = min(items, tid * per), i1 = min(items, i0 + per);
     int64_t sum = 0;
     for (int i = i0; i < i1; ++i) {
-        const int t = group_of(a, i, 0, report).tiles, u = t ? t + GROUP_COST : 0;
+        const Group g = group_of(a, i, 0, report);
+        const int64_t u = g.steps ? ((int64_t)g.steps * step_cost(a, g.rows) + GROUP_COST) * head_steps(a, g.rows) : 0;
         prefix[i] = u; sum += u;
     }
     int64_t incl = sum;
@@ -242,9 +252,9 @@ __device__ Plan make_plan(const AttendArgs& a, int64_t* prefix, int64_t* scan, i
     if (tid == 0) prefix[items] = all;
     __syncthreads();
     Plan p;
-    p.total = all * a.n_kv_heads;
-    // a share holds at least one tile of every group that begins before it and ends behind it
-    p.shares = (int)min((int64_t)n_blocks, max((int64_t)1, p.total / (GROUP_COST + 1)));
+    p.total = all;
+    // a share holds at least one step of every group that begins before it and ends behind it
+    p.shares = (int)min((int64_t)n_blocks, max((int64_t)1, p.total / (GROUP_COST + BOTH_COST)));
     return p;
 }
 
@@ -263,29 +273,31 @@ __device__ __forceinline__ Walk begin_walk(const AttendArgs& a, const Plan& p, i
     }
     return w;
 }
-// The next group that has tiles here: tiles [*t0, *t1) of it.  False at the end.  *start: unit of its first tile.
+// The next group that has steps here: steps [*t0, *t1) of it.  False at the end.  *start: unit of its first step.
 __device__ __forceinline__ bool next_group(const AttendArgs& a, const int64_t* prefix, Walk& w, Group* g, int* t0, int* t1, int64_t* start) {
     const int items = a.n * a.row_tiles;
     while (w.unit < w.end) {
         if (!a.planned) {
-            *g = group_of(a, (int)(w.unit / a.n_kv_heads), (int)(w.unit % a.n_kv_heads), true);
+            const int head = (int)(w.unit % a.n_kv_heads);
+            *g = group_of(a, (int)(w.unit / a.n_kv_heads), head, true);
             w.unit += w.step;
-            *t0 = 0; *t1 = g->tiles; *start = 0;
-            if (g->tiles) return true;
+            *t0 = 0; *t1 = g->steps; *start = 0;
+            if (g->steps && (g->rows > TILE_ROWS || head % 2 == 0)) return true;
             continue;
         }
         const int64_t u = w.unit;
         int lo = 0, hi = items;      // last item whose units begin at or before u (items without any are passed over)
-        while (hi - lo > 1) { const int m = (lo + hi) >> 1; if (prefix[m] * a.n_kv_heads <= u) lo = m; else hi = m; }
-        const int64_t units = prefix[lo + 1] - prefix[lo], in = u - prefix[lo] * a.n_kv_heads;
-        const int head = (int)(in / units);
-        const int64_t x = in - head * units, left = min(units - x, w.end - u);
+        while (hi - lo > 1) { const int m = (lo + hi) >> 1; if (prefix[m] <= u) lo = m; else hi = m; }
+        *g = group_of(a, lo, 0);
+        const int steps = head_steps(a, g->rows);
+        const int64_t units = (prefix[lo + 1] - prefix[lo]) / steps, in = u - prefix[lo];
+        const int at = (int)(in / units);
+        const int64_t x = in - at * units, left = min(units - x, w.end - u);
         w.unit = u + left;
-        *t0 = (int)max((int64_t)0, x - GROUP_COST);
-        *t1 = (int)max((int64_t)0, x + left - GROUP_COST);
-        if (*t1 <= *t0) continue;
-        *g = group_of(a, lo, head);
-        *t1 = min(*t1, g->tiles);    // the lengths may not change while the call runs; never behind the group all the same
+        if (at) *g = group_of(a, lo, g->rows > TILE_ROWS ? at : 2 * at);
+        const int cost = step_cost(a, g->rows);             // step i belongs to the share of unit GROUP_COST + i * cost
+        *t0 = (int)((max((int64_t)0, x - GROUP_COST) + cost - 1) / cost);
+        *t1 = min((int)((max((int64_t)0, x + left - GROUP_COST) + cost - 1) / cost), g->steps);
         *start = u - x + GROUP_COST;
         if (*t1 > *t0) return true;
     }
@@ -295,7 +307,7 @@ __device__ __forceinline__ bool next_group(const AttendArgs& a, const int64_t* p
 // A group as the roles of the block see it.
 struct Seg {
     Group g;
-    int t0, t1;                      // its tiles here; t1 = t0: no more groups
+    int t0, t1;                      // its steps here; t1 = t0: no more groups
     uint4 anc[HX_TREE_MAX];          // tree: the ancestors of every drafted token, as bits; none for one that is not there
 };
 
@@ -358,17 +370,33 @@ __device__ __forceinline__ int row_of(const AttendArgs& a, const Group& g, int x
 // Entries of [0, 32) below n, as bits.
 __device__ __forceinline__ uint32_t below(int n) { return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u; }
 
-// What row r of the group sees of the 32 W entries from xa on, as bits (entries behind the axis are the caller's to take out).
-template <int W>
-__device__ __forceinline__ void sees(const AttendArgs& a, const Group& g, const uint4* anc, int r, int xa, uint32_t (&m)[W]) {
+// What a row sees of its group's axis.  Window: entries below `first`, and [lo, hi).  Tree: entries below lo (`first` = 0: the token is
+// not there and sees nothing), and its ancestors among the drafted ones from lo on.
+struct View { int first, lo, hi; uint4 anc; };
+__device__ __forceinline__ View view_of(const AttendArgs& a, const Group& g, const uint4* anc, int r) {
     const int qi = (g.r0 + r) / a.group;
+    View v;
+    v.anc = make_uint4(0, 0, 0, 0);
     if (a.tree) {
-        const uint4 t = anc[qi];
-        const bool there = (t.x | t.y | t.z | t.w) != 0;
-        const uint32_t w[5] = {t.x, t.y, t.z, t.w, 0u};
+        v.anc = anc[qi];
+        v.first = (v.anc.x | v.anc.y | v.anc.z | v.anc.w) != 0;
+        v.lo = g.axis.n_sink; v.hi = 0;
+        return v;
+    }
+    const int p = g.len - g.nq + qi, gap = g.axis.gap;
+    v.first = min(a.sinks, p + 1);
+    if (gap) v.first = min(v.first, g.axis.n_sink);
+    v.lo = max(p - a.window + 1 - gap, g.axis.n_sink); v.hi = p + 1 - gap;
+    return v;
+}
+// The 32 W entries from xa on, as bits (entries behind the axis are the caller's to take out).
+template <int W>
+__device__ __forceinline__ void sees(int tree, const View& v, int xa, uint32_t (&m)[W]) {
+    if (tree) {
+        const uint32_t w[5] = {v.anc.x, v.anc.y, v.anc.z, v.anc.w, 0u};
 #pragma unroll
         for (int i = 0; i < W; ++i) {
-            const int s = xa + 32 * i - g.axis.n_sink;           // drafted token of the word's first bit
+            const int s = xa + 32 * i - v.lo;            // drafted token of the word's first bit
             uint32_t x = 0;
             if (s <= -32) x = 0xffffffffu;
             else if (s < 0) x = below(-s) | w[0] << -s;
@@ -376,54 +404,73 @@ __device__ __forceinline__ void sees(const AttendArgs& a, const Group& g, const 
 #pragma unroll
                 for (int k = 0; k < 4; ++k) if ((s >> 5) == k) x = __funnelshift_r(w[k], w[k + 1], s & 31);
             }
-            m[i] = there ? x : 0u;
+            m[i] = v.first ? x : 0u;
         }
         return;
     }
-    const int p = g.len - g.nq + qi, gap = g.axis.gap;
-    int first = min(a.sinks, p + 1);                     // first tokens: entries below this
-    if (gap) first = min(first, g.axis.n_sink);
-    first -= xa;
-    const int lo = max(p - a.window + 1 - gap, g.axis.n_sink) - xa, hi = p + 1 - gap - xa;
 #pragma unroll
-    for (int i = 0; i < W; ++i) m[i] = below(first - 32 * i) | (below(hi - 32 * i) & ~below(lo - 32 * i));
+    for (int i = 0; i < W; ++i) m[i] = below(v.first - xa - 32 * i) | (below(v.hi - xa - 32 * i) & ~below(v.lo - xa - 32 * i));
 }
 
 template <int D> struct Shape {
     static constexpr int CHUNKS = D / 8;                       // 16-byte pieces of a row
     static constexpr int PANELS = (D + 63) / 64;               // of 128 bytes
-    static constexpr int TILE = PANELS * 128 * 128;            // bytes of K, or V, of a tile, and of 128 rows of Q
-    static constexpr int SLOTS = PANELS == 1 ? 8 : 4;          // 128 KB of keys and values in flight
-    static constexpr int SMEM = 2 * TILE + SLOTS * TILE + 1024;
+    static constexpr int TILE = PANELS * 128 * 128;            // bytes of 128 rows of Q
+    static constexpr int SLOT = PANELS * 64 * 128;             // of K, or V, of a step
+    static constexpr int SLOTS = 8 * 16384 / SLOT;             // 128 KB of keys and values in flight
+    static constexpr int SMEM = 2 * TILE + SLOTS * SLOT + 1024;
 };
-// Byte of piece c of row r of a tile.
-__device__ __forceinline__ uint32_t piece(int r, int c) { return (uint32_t)((c >> 3) * 16384 + r * 128 + (((c & 7) ^ (r & 7)) << 4)); }
+// Byte of piece c of row r of a tile whose panels hold `rows` rows.
+__device__ __forceinline__ uint32_t piece(int r, int c, int rows) { return (uint32_t)((c >> 3) * rows * 128 + r * 128 + (((c & 7) ^ (r & 7)) << 4)); }
 
 struct Shared {
     Seg seg[SEGS];
     int64_t prefix[PLAN_ITEMS + 1];
     int64_t scan[THREADS / 32];
-    alignas(16) uint32_t valid[VALID_RING][4];   // entries of a tile that have a row
-    float2 stat[TILE_ROWS];          // maximum and sum of the second stream, where it shares its rows
-    float buf[2][TILE_ROWS * 17];    // 16 columns of every copy's result
+    alignas(16) uint32_t valid[2][VALID_RING][2];        // entries of a step that have a row, of each of two heads
+    float2 stat[2][TILE_ROWS];          // maximum and sum of the second stream, where it shares its rows
+    alignas(16) float buf[8 * 512];  // results on their way out, 2 KB to a warp; a stream's four also join the copies of rows
+    float fin[2][TILE_ROWS / 2];     // what the rows' sums are multiplied by
     int link[HX_TREE_MAX];
-    int4 rows[4][32];                // row numbers of the tiles being loaded, four to a lane; -1: zeros
-    unsigned long long full[8], empty[8], q_full, q_empty, s_full[2][2], p_full[2][2], pv[2], o_full[2], x_ready, x_free, join, seg_full[SEGS], seg_empty[SEGS], drained[2];
+    unsigned long long full[16], empty[16], q_full, q_empty, s_full[2][2], p_full[2][2], pv[2], o_full[2], x_ready, x_free, join[2], seg_full[SEGS], seg_empty[SEGS], drained[2];
     uint32_t tmem;
     int quit;
 };
 
-// Places of tile j's keys and values in the order in which a group of n tiles is loaded.
-__device__ __forceinline__ int key_place(bool pair, int n, int j) { return pair ? 2 * j : j == 0 ? 0 : 2 * j - 1; }
-__device__ __forceinline__ int value_place(bool pair, int n, int j) { return pair ? 2 * j + 1 : j + 1 < n ? 2 * j + 2 : 2 * n - 1; }
+// How a group is shared by the streams: 128 rows each of the same head, the same rows of two heads, or alternate steps of one.
+enum Mode { ROWS, HEADS, STEPS };
+__device__ __forceinline__ Mode mode_of(const Group& g) { return g.rows > TILE_ROWS ? ROWS : g.heads == 2 ? HEADS : STEPS; }
+// Loads of a group come in the order in which the products need them: the keys of the first `lead` steps (two to a stream), then values
+// of a step and keys of the step `lead` ahead, in turn; of two heads, one behind the other.  Places of step i's for stream s among n:
+__device__ __forceinline__ int lead_of(Mode m) { return m == STEPS ? 4 : 2; }
+__device__ __forceinline__ int loads_of(Mode m, int n) { return m == HEADS ? 4 * n : 2 * n; }
+__device__ __forceinline__ int key_place(Mode m, int i, int s) {
+    const int at = i < lead_of(m) ? i : 2 * i - lead_of(m) + 1;
+    return m == HEADS ? 2 * at + s : at;
+}
+__device__ __forceinline__ int value_place(Mode m, int n, int i, int s) {
+    const int at = min(n, lead_of(m) + i) + i;
+    return m == HEADS ? 2 * at + s : at;
+}
+
+struct Load { bool keys; int step, head; };
+// Load number o of a group of n steps.
+__device__ __forceinline__ Load load_at(Mode m, int n, int o) {
+    Load l;
+    l.head = m == HEADS ? o & 1 : 0;
+    const int at = m == HEADS ? o >> 1 : o, lead = min(lead_of(m), n), q = at - lead, turns = 2 * (n - lead);
+    l.keys = q < 0 || (q < turns && (q & 1));
+    l.step = q < 0 ? at : q < turns ? (q >> 1) + (q & 1 ? lead : 0) : q - (n - lead);
+    return l;
+}
 
 struct Maps { CUtensorMap k, v, k_draft, v_draft; };     // rows of tokens: of the cache's layer, and drafted ones
 
-// Where row r of a group goes: element of out, element of lse.
+// Where row r of a group goes, of KV head `head`: element of out, element of lse.
 struct Place { int64_t out, lse; };
-__device__ __forceinline__ Place place_of(const AttendArgs& a, const Group& g, int r) {
-    const int qi = (g.r0 + r) / a.group, head = g.head * a.group + g.r0 + r - qi * a.group;
-    return Place{(int64_t)(g.row0 + qi) * a.o_row + (int64_t)head * a.o_head, (int64_t)(g.row0 + qi) * a.n_kv_heads * a.group + head};
+__device__ __forceinline__ Place place_of(const AttendArgs& a, const Group& g, int head, int r) {
+    const int qi = (g.r0 + r) / a.group, h = head * a.group + g.r0 + r - qi * a.group;
+    return Place{(int64_t)(g.row0 + qi) * a.o_row + (int64_t)h * a.o_head, (int64_t)(g.row0 + qi) * a.n_kv_heads * a.group + h};
 }
 
 template <int N> struct Columns { static constexpr int value = N; };
@@ -470,7 +517,6 @@ __device__ __forceinline__ bool softmax_step(uint32_t S_at, uint32_t O_at, int c
         }
     }
     const float safe = mx == -INFINITY ? 0.f : mx;
-    float s4[4] = {0.f, 0.f, 0.f, 0.f};
     if constexpr (NC < STEP) {
         const uint32_t zeros[16] = {};
 #pragma unroll
@@ -478,6 +524,7 @@ __device__ __forceinline__ bool softmax_step(uint32_t S_at, uint32_t O_at, int c
             if (c != col / 2) { if constexpr (NC == 16) tc_st8(S_at + c, zeros); else tc_st16(S_at + c, zeros); }
     }
     constexpr int G = NC < 32 ? NC : 32;
+    float s4[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int k = 0; k < NC; k += G) {
         uint32_t w[G / 2];
@@ -517,8 +564,8 @@ __global__ void __launch_bounds__(THREADS, 1) hx_attend_kernel(const AttendArgs 
             for (int h = 0; h < 2; ++h) { bar_init(smem_at(&sh.s_full[i][h]), 1); bar_init(smem_at(&sh.p_full[i][h]), 4); }
             bar_init(smem_at(&sh.pv[i]), 1); bar_init(smem_at(&sh.o_full[i]), 1);
         }
-        bar_init(smem_at(&sh.x_ready), 4); bar_init(smem_at(&sh.x_free), 4); bar_init(smem_at(&sh.join), 4);
-        for (int i = 0; i < SEGS; ++i) { bar_init(smem_at(&sh.seg_full[i]), 1); bar_init(smem_at(&sh.seg_empty[i]), 11); }
+        bar_init(smem_at(&sh.x_ready), 4); bar_init(smem_at(&sh.x_free), 4); bar_init(smem_at(&sh.join[0]), 4); bar_init(smem_at(&sh.join[1]), 4);
+        for (int i = 0; i < SEGS; ++i) { bar_init(smem_at(&sh.seg_full[i]), 1); bar_init(smem_at(&sh.seg_empty[i]), LOADERS + 2 + 8); }
         bar_init(smem_at(&sh.drained[0]), 1); bar_init(smem_at(&sh.drained[1]), 1);
         sh.quit = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -532,160 +579,142 @@ __global__ void __launch_bounds__(THREADS, 1) hx_attend_kernel(const AttendArgs 
     tc_after();
     const uint32_t tmem = sh.tmem;
 
-    if (role == 2) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
-        if (warp == 8) {
-            bool go = true;
-            // ---- keys and values
-            int kvn = 0, tiles_seen = 0;
-            for (int n = 0; go; ++n) {
-                const int si = n % SEGS;
-                if (!(go = warp_wait(smem_at(&sh.seg_full[si]), (n / SEGS) & 1, quit))) break;
-                const Group g = sh.seg[si].g;
-                const int t0 = sh.seg[si].t0, nt = sh.seg[si].t1 - t0;
-                __syncwarp();
-                if (lane == 0) bar_arrive(smem_at(&sh.seg_empty[si]));
-                if (nt <= 0) break;
-                const bool pair = g.rows > TILE_ROWS;
-                const int per = max(a.chunk, 4);         // a lane's entries: drafted or cached together
-                const bool mine = lane * per < BN;
-                // the lane's entry of the page table for tile j, -1 where there is none: read one tile ahead of its use
-                auto entry = [&](int j) {
-                    const int x = (t0 + j) * BN + lane * per;
-                    if (a.chunk < 4 || !mine || j >= nt || x >= (a.tree ? g.len : g.axis.n)) return -1;
-                    const int c = (a.tree ? x : hx_axis_pos(g.axis, x)) / a.page_tokens;
-                    return c < a.max_pages ? a.table[(int64_t)g.seq * a.max_pages + c] : -1;
-                };
-                int next = entry(0);
-                for (int o = 0; o < 2 * nt; ++o) {
-                    bool keys; int j;                    // place o of the order: which tile, keys or values
-                    if (pair) { keys = !(o & 1); j = o >> 1; }
-                    else if (o == 0) { keys = true; j = 0; }
-                    else if (o == 2 * nt - 1) { keys = false; j = nt - 1; }
-                    else { keys = o & 1; j = keys ? (o + 1) >> 1 : (o - 2) >> 1; }
-                    const int x = (t0 + j) * BN + lane * per;
-                    bool drafted = a.tree && x >= g.axis.n_sink;
-                    int4 rows = make_int4(-BN, -BN, -BN, -BN);           // rows ahead of the map: zeros
-                    if (keys) {
-                        uint32_t bits = 0;
-                        if (a.chunk < 4) {
-                            rows.x = row_of(a, g, x, &drafted); rows.y = row_of(a, g, x + 1, &drafted);
-                            rows.z = row_of(a, g, x + 2, &drafted); rows.w = row_of(a, g, x + 3, &drafted);
-                            bits = (uint32_t)(rows.x >= 0) | (uint32_t)(rows.y >= 0) << 1 | (uint32_t)(rows.z >= 0) << 2 | (uint32_t)(rows.w >= 0) << 3;
-                        } else {
-                            const int page = next, end = a.tree && !drafted ? g.len : g.axis.n;
-                            next = entry(j + 1);
-                            int n_have = mine ? max(0, min(per, end - x)) : 0;       // rows of the chunk that are entries of the axis
-                            if (drafted) rows.x = g.row0 + x - g.axis.n_sink;
-                            else if (n_have > 0 && page >= 0 && page < a.n_pages) rows.x = page * a.page_rows + (a.tree ? x : hx_axis_pos(g.axis, x)) % a.page_tokens;
-                            else if (n_have > 0) { n_have = 0; atomicExch(a.status, HX_ERR_INVALID_ARG); }
-                            n_have = __shfl_sync(0xffffffffu, n_have, 4 * lane / per);
-                            bits = below(n_have - 4 * lane % per) & 15u;
-                        }
-                        bits <<= 4 * (lane & 7);
-#pragma unroll
-                        for (int k = 1; k < 8; k *= 2) bits |= __shfl_xor_sync(0xffffffffu, bits, k);
-                        if ((lane & 7) == 0) sh.valid[(tiles_seen + j) % VALID_RING][lane >> 3] = bits;
-                        sh.rows[(tiles_seen + j) & 3][lane] = rows;
-                    } else {
-                        rows = sh.rows[(tiles_seen + j) & 3][lane];          // written by this lane
-                    }
-                    const int slot = kvn % NS;
-                    const uint32_t bar = smem_at(&sh.full[slot]), to = smem_at(kv_s + slot * S::TILE) + lane * per * 128;
-                    if (!(go = warp_wait(smem_at(&sh.empty[slot]), ((kvn / NS) & 1) ^ 1, quit))) break;
-                    if (lane == 0) bar_expect(bar, S::TILE);
-                    __syncwarp();
-                    const CUtensorMap* map = drafted ? (keys ? &maps.k_draft : &maps.v_draft) : (keys ? &maps.k : &maps.v);
-                    if (mine) {
-#pragma unroll
-                        for (int p = 0; p < S::PANELS; ++p) {
-                            if (a.chunk < 4) gather4(to + p * 16384, map, g.head * D + p * 64, rows, bar);
-                            else load_box(to + p * 16384, map, g.head * D + p * 64, rows.x, bar);
-                        }
-                    }
-                    ++kvn;
+    if (role == 3) {
+        // ---- keys and values
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+        bool go = true;
+        int kvn = 0, seen = 0;                           // loads and steps of the groups before
+        for (int n = 0; go; ++n) {
+            const int si = n % SEGS;
+            if (!(go = warp_wait(smem_at(&sh.seg_full[si]), (n / SEGS) & 1, quit))) break;
+            const Group g = sh.seg[si].g;
+            const int t0 = sh.seg[si].t0, nt = sh.seg[si].t1 - t0;
+            __syncwarp();
+            if (lane == 0) bar_arrive(smem_at(&sh.seg_empty[si]));
+            if (nt <= 0) break;
+            const Mode mode = mode_of(g);
+            const int per = max(a.chunk, 4);             // a lane's entries: drafted or cached together
+            const bool mine = lane * per < STEP;
+            // the lane's entry of the page table for a step, -1 where there is none: read one load ahead of its use
+            auto entry = [&](int i) {
+                const int x = (t0 + i) * STEP + lane * per;
+                if (a.chunk < 4 || !mine || i >= nt || x >= (a.tree ? g.len : g.axis.n)) return -1;
+                const int c = (a.tree ? x : hx_axis_pos(g.axis, x)) / a.page_tokens;
+                return c < a.max_pages ? a.table[(int64_t)g.seq * a.max_pages + c] : -1;
+            };
+            const int total = loads_of(mode, nt);
+            int o = ((warp & 3) - kvn) & (LOADERS - 1), next = entry(load_at(mode, nt, o).step);
+            for (; o < total; o += LOADERS) {
+                const Load load = load_at(mode, nt, o);
+                const int i = load.step, x = (t0 + i) * STEP + lane * per, page = next;
+                next = entry(load_at(mode, nt, o + LOADERS).step);
+                const bool drafted = a.tree && x >= g.axis.n_sink;
+                int4 rows = make_int4(-STEP, -STEP, -STEP, -STEP);       // rows ahead of the map: zeros
+                uint32_t bits = 0;                       // of the lane's four entries
+                if (a.chunk < 4) {
+                    bool d;
+                    if (mine) { rows.x = row_of(a, g, x, &d); rows.y = row_of(a, g, x + 1, &d); rows.z = row_of(a, g, x + 2, &d); rows.w = row_of(a, g, x + 3, &d); }
+                    bits = (uint32_t)(rows.x >= 0) | (uint32_t)(rows.y >= 0) << 1 | (uint32_t)(rows.z >= 0) << 2 | (uint32_t)(rows.w >= 0) << 3;
+                } else {
+                    int n_have = mine ? max(0, min(per, (a.tree && !drafted ? g.len : g.axis.n) - x)) : 0;       // rows of the chunk that are entries of the axis
+                    if (drafted) rows.x = g.row0 + x - g.axis.n_sink;
+                    else if (n_have > 0 && page >= 0 && page < a.n_pages) rows.x = page * a.page_rows + (a.tree ? x : hx_axis_pos(g.axis, x)) % a.page_tokens;
+                    else if (n_have > 0) { n_have = 0; atomicExch(a.status, HX_ERR_INVALID_ARG); }
+                    n_have = __shfl_sync(0xffffffffu, n_have, (lane & 15) * 4 / per);
+                    bits = below(n_have - (lane & 15) * 4 % per) & 15u;
                 }
-                tiles_seen += nt;
+                const int at = kvn + o, slot = at % NS;
+                const uint32_t bar = smem_at(&sh.full[slot]), to = smem_at(kv_s + slot * S::SLOT) + lane * per * 128;
+                if (!(go = warp_wait(smem_at(&sh.empty[slot]), ((at / NS) & 1) ^ 1, quit))) break;
+                if (load.keys) {
+                    bits <<= 4 * (lane & 7);
+#pragma unroll
+                    for (int k = 1; k < 8; k *= 2) bits |= __shfl_xor_sync(0xffffffffu, bits, k);
+                    if (lane == 0 || lane == 8) sh.valid[load.head][(seen + i) % VALID_RING][lane >> 3] = bits;
+                    __syncwarp();
+                }
+                if (lane == 0) bar_expect(bar, S::SLOT);
+                __syncwarp();
+                const CUtensorMap* map = drafted ? (load.keys ? &maps.k_draft : &maps.v_draft) : (load.keys ? &maps.k : &maps.v);
+                if (mine) {
+#pragma unroll
+                    for (int p = 0; p < S::PANELS; ++p) {
+                        if (a.chunk < 4) gather4(to + p * 8192, map, (g.head + load.head) * D + p * 64, rows, bar);
+                        else load_box(to + p * 8192, map, (g.head + load.head) * D + p * 64, rows.x, bar);
+                    }
+                }
             }
-            // copies that are on their way end before the block does
-            for (int i = 0; i < NS && !go; ++i) {
-                const int at = kvn - 1 - i;
-                if (at >= 0) { const unsigned long long t0 = now_ns(); while (!bar_try(smem_at(&sh.full[at % NS]), (at / NS) & 1) && now_ns() - t0 < WAIT_NS) { } }
-            }
-        } else if (warp < 11) {
+            kvn += total;
+            seen += nt;
+        }
+        if (!go) {                                       // copies that are on their way end before the block does
+            const unsigned long long since = now_ns();
+            while (now_ns() - since < WAIT_NS / 100) { }
+        }
+    } else if (role == 2) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+        if (warp < 10) {
             // ---- products of one stream
             constexpr uint32_t QK = product(Elem<T>::FORMAT, STEP, false), PV = product(Elem<T>::FORMAT, D, true);
-            const int s = warp - 9;
-            const uint32_t q_m = matrix(smem_at(q_s), 16), k_m = matrix(smem_at(kv_s), 16), v_m = matrix(smem_at(kv_s), 16384);
+            const int s = warp - 8;
+            const uint32_t q_m = matrix(smem_at(q_s), 16), k_m = matrix(smem_at(kv_s), 16), v_m = matrix(smem_at(kv_s), 8192);
             const uint32_t S_at = uniform(tmem + s * 128), O_at = uniform(tmem + 256 + s * 128);
-            int kvn = 0, pn = 0;
+            int kvn = 0, sn = 0;                         // loads before the group, steps of this stream so far
             bool go = true;
             for (int n = 0; go; ++n) {
                 const int si = n % SEGS;
                 if (!(go = warp_wait(smem_at(&sh.seg_full[si]), (n / SEGS) & 1, quit))) break;
                 const int nt = sh.seg[si].t1 - sh.seg[si].t0;
-                const bool pair = sh.seg[si].g.rows > TILE_ROWS;
+                const Mode mode = mode_of(sh.seg[si].g);
                 __syncwarp();
                 if (lane == 0) bar_arrive(smem_at(&sh.seg_empty[si]));
                 if (nt <= 0) break;
                 if (!(go = warp_wait(smem_at(&sh.q_full), n & 1, quit))) break;
-                const uint32_t q_t = uniform(q_m + (pair ? s : 0) * (S::TILE >> 4));
-                const int step = pair ? 1 : 2, mine = pair ? 0 : s;          // this stream's tiles: mine, mine + step, ...
+                const uint32_t q_t = uniform(q_m + (mode == STEPS ? 0 : s) * (S::TILE >> 4));
+                const int step = mode == STEPS ? 2 : 1, mine = mode == STEPS ? s : 0;          // this stream's steps: mine, mine + step, ...
                 // a slot, and q, is given back by both streams, or twice by the one that reads it alone
                 auto give_back = [&](uint32_t bar, bool twice) { tc_commit(bar); if (twice) tc_commit(bar); };
-                auto ready = [&](int at) { return warp_wait(smem_at(&sh.full[at % NS]), (at / NS) & 1, quit); };
-                // scores of half h of the tile in `slot`; done: no products after these read q
-                auto scores = [&](int slot, int h, bool done) {
-                    const uint32_t k_t = uniform(k_m + slot * (S::TILE >> 4) + h * 512), to = S_at + h * STEP;
+                auto ready = [&](int at) {
+                    if (!warp_wait(smem_at(&sh.full[at % NS]), (at / NS) & 1, quit)) return false;
+                    tc_after();
+                    return true;
+                };
+                // scores of step i, this stream's number k: into buffer k & 1
+                auto scores = [&](int i, int k) {
+                    const int at = kvn + key_place(mode, i, s), slot = at % NS;
+                    if (!ready(at)) return false;
+                    const uint32_t k_t = uniform(k_m + slot * (S::SLOT >> 4)), to = uniform(S_at + (k & 1) * STEP);
                     if (elect()) {
 #pragma unroll
                         for (int ks = 0; ks < D / 16; ++ks)
-                            tc_mma_ss(to, q_t + (ks >> 2) * 1024 + (ks & 3) * 2, k_t + (ks >> 2) * 1024 + (ks & 3) * 2, QK, ks > 0);
-                        tc_commit(smem_at(&sh.s_full[s][h]));
-                        if (h == 1) {
-                            give_back(smem_at(&sh.empty[slot]), !pair);
-                            if (done) give_back(smem_at(&sh.q_empty), nt == 1 && !pair);
-                        }
+                            tc_mma_ss(to, q_t + (ks >> 2) * 1024 + (ks & 3) * 2, k_t + (ks >> 2) * 512 + (ks & 3) * 2, QK, ks > 0);
+                        tc_commit(smem_at(&sh.s_full[s][k & 1]));
+                        give_back(smem_at(&sh.empty[slot]), mode != ROWS);
+                        if (i + step >= nt) give_back(smem_at(&sh.q_empty), nt == 1 && mode == STEPS);       // no products after these read q
                     }
                     __syncwarp();
+                    return true;
                 };
-                // weights of half h of the tile in `slot` times its values; first, last: of this stream's tiles
-                auto values = [&](int slot, int h, bool first, bool last) {
-                    const uint32_t v_t = uniform(v_m + slot * (S::TILE >> 4) + h * 512), from = S_at + h * STEP;
+                // weights of step i, number k, times its values
+                auto values = [&](int i, int k) {
+                    const int at = kvn + value_place(mode, nt, i, s), slot = at % NS;
+                    if (!ready(at) || !warp_wait(smem_at(&sh.p_full[s][k & 1]), (k >> 1) & 1, quit)) return false;
+                    tc_after();
+                    const uint32_t v_t = uniform(v_m + slot * (S::SLOT >> 4)), from = uniform(S_at + (k & 1) * STEP);
                     if (elect()) {
 #pragma unroll
-                        for (int ks = 0; ks < STEP / 16; ++ks) tc_mma_ts(O_at, from + ks * 8, v_t + ks * 128, PV, !(first && h == 0 && ks == 0));
+                        for (int ks = 0; ks < STEP / 16; ++ks) tc_mma_ts(O_at, from + ks * 8, v_t + ks * 128, PV, !(i == mine && ks == 0));
                         tc_commit(smem_at(&sh.pv[s]));
-                        if (h == 1) {
-                            give_back(smem_at(&sh.empty[slot]), !pair);
-                            if (last) tc_commit(smem_at(&sh.o_full[s]));
-                        }
+                        give_back(smem_at(&sh.empty[slot]), mode != ROWS);
+                        if (i + step >= nt) tc_commit(smem_at(&sh.o_full[s]));
                     }
                     __syncwarp();
+                    return true;
                 };
-                if (mine < nt) {
-                    const int at = kvn + key_place(pair, nt, mine);
-                    if (!(go = ready(at))) break;
-                    tc_after();
-                    scores(at % NS, 0, false);
-                    scores(at % NS, 1, mine + step >= nt);
-                }
-                for (int j = mine; j < nt && go; j += step) {
-                    const int v_at = kvn + value_place(pair, nt, j), next = j + step, k_at = kvn + key_place(pair, nt, next);
-                    if (!(go = ready(v_at))) break;
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        if (!(go = warp_wait(smem_at(&sh.p_full[s][h]), pn & 1, quit))) break;
-                        tc_after();
-                        values(v_at % NS, h, j == mine, next >= nt);
-                        if (next < nt) {
-                            if (h == 0) { if (!(go = ready(k_at))) break; tc_after(); }
-                            scores(k_at % NS, h, next + step >= nt);
-                        }
-                    }
-                    ++pn;
-                }
-                kvn += 2 * nt;
+                for (int k = 0; k < 2 && mine + k * step < nt; ++k) go = go && scores(mine + k * step, sn + k);
+                for (int i = mine; i < nt && go; i += step, ++sn)
+                    go = values(i, sn) && (i + 2 * step >= nt || scores(i + 2 * step, sn + 2));
+                kvn += loads_of(mode, nt);
             }
             if (!go) {                                   // what was issued ends before the tensor memory is given back
                 if (elect()) tc_commit(smem_at(&sh.drained[s]));
@@ -693,7 +722,7 @@ __global__ void __launch_bounds__(THREADS, 1) hx_attend_kernel(const AttendArgs 
                 const unsigned long long t0 = now_ns();
                 while (!bar_try(smem_at(&sh.drained[s]), 0) && now_ns() - t0 < WAIT_NS) { }
             }
-        } else {
+        } else if (warp == 10) {
             // ---- groups, and their rows of q
             Walk w = begin_walk(a, plan, blockIdx.x, gridDim.x);
             for (int n = 0;; ++n) {
@@ -708,24 +737,24 @@ __global__ void __launch_bounds__(THREADS, 1) hx_attend_kernel(const AttendArgs 
                 if (lane == 0) {
                     if (more) seg.g = g;
                     seg.t0 = more ? t0 : 0; seg.t1 = more ? t1 : 0;
-                    if (more && a.planned && t0 == 0 && t1 < g.tiles)        // the shares that hold the rest of the group follow this one
-                        a.desc[blockIdx.x] = make_int4(hx_share_of(plan.total, start + g.tiles - 1, plan.shares) - (int)blockIdx.x + 1, g.item, g.head, 0);
+                    if (more && a.planned && t0 == 0 && t1 < g.steps)        // the shares that hold the rest of the group follow this one
+                        a.desc[blockIdx.x] = make_int4(hx_share_of(plan.total, start + (int64_t)(g.steps - 1) * step_cost(a, g.rows), plan.shares) - (int)blockIdx.x + 1, g.item, g.head, 0);
                 }
                 __syncwarp();
                 if (lane == 0) bar_arrive(smem_at(&sh.seg_full[si]));
                 if (!more) break;
                 if (!warp_wait(smem_at(&sh.q_empty), (n & 1) ^ 1, quit)) break;
-                const int head0 = g.head * a.group, copies = copies_of(g.rows), room = TILE_ROWS / copies;
-                for (int rb = 0; rb < (copies > 1 ? TILE_ROWS : g.rows); rb += 32) {         // 32 rows of the tile, a lane finds the place of each
-                    const int r = copies > 1 ? (rb + lane) & (room - 1) : rb + lane;
+                const int copies = copies_of(g.rows), room = TILE_ROWS / copies, blocks = copies > 1 ? 4 : (g.rows + 31) / 32;
+                for (int b = 0; b < blocks * g.heads; ++b) {         // 32 rows of the tile, a lane finds the place of each; two heads have a tile each
+                    const int t = b / blocks, rb = (b - t * blocks) * 32, r = copies > 1 ? (rb + lane) & (room - 1) : rb + lane;
                     const int qi = r < g.rows ? (g.r0 + r) / a.group : 0, hd = r < g.rows ? g.r0 + r - qi * a.group : 0;
-                    const unsigned long long src = reinterpret_cast<unsigned long long>(a.q + 2 * ((int64_t)(g.row0 + qi) * a.q_row + (int64_t)(head0 + hd) * a.q_head));
+                    const unsigned long long src = reinterpret_cast<unsigned long long>(a.q + 2 * ((int64_t)(g.row0 + qi) * a.q_row + (int64_t)((g.head + t) * a.group + hd) * a.q_head));
 #pragma unroll 8
                     for (int i = 0; i < S::CHUNKS; ++i) {
-                        const int e = i * 32 + lane, q = e / S::CHUNKS, c = e - q * S::CHUNKS, rr = rb + q;
+                        const int e = i * 32 + lane, q = e / S::CHUNKS, c = e - q * S::CHUNKS, rr = t * TILE_ROWS + rb + q;
                         const int have = __shfl_sync(0xffffffffu, r < g.rows, q);
                         const char* from = reinterpret_cast<const char*>(__shfl_sync(0xffffffffu, src, q));
-                        copy16(smem_at(q_s + (rr >> 7) * S::TILE) + piece(rr & 127, c), from + c * 16, have ? 16 : 0);
+                        copy16(smem_at(q_s + (rr >> 7) * S::TILE) + piece(rr & 127, c, 128), from + c * 16, have ? 16 : 0);
                     }
                 }
                 copies_wait();
@@ -735,11 +764,11 @@ __global__ void __launch_bounds__(THREADS, 1) hx_attend_kernel(const AttendArgs 
         }
     } else {
         // ---- softmax
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");     // 2 x 208 + 88 = the 3 x 168 of the launch
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 192;");     // 2 x 192 + 2 x 64 = the 4 x 128 of the launch
         const int s = role, row = tid & 127;
         const uint32_t lanes = (uint32_t)(warp & 3) << 21;       // the warp's quarter of the 128 lanes
         const uint32_t S_at = tmem + lanes + s * 128, O_at = tmem + lanes + 256;
-        int sn = 0, on = 0, xn = 0, jn = 0, kvn = 0, tiles_seen = 0;     // sn: tiles of this stream
+        int sn = 0, on = 0, xn = 0, jn = 0, kvn = 0, before = 0;         // sn: steps of this stream; before: steps of the groups before
         bool go = true, odd = false;
         for (int n = 0; go; ++n) {
             const int si = n % SEGS;
@@ -748,94 +777,95 @@ __global__ void __launch_bounds__(THREADS, 1) hx_attend_kernel(const AttendArgs 
             const int t0 = seg.t0, nt = seg.t1 - t0;
             if (nt <= 0) break;
             const Group& g = seg.g;
-            const bool pair = g.rows > TILE_ROWS;
-            const int copies = copies_of(g.rows);
+            const Mode mode = mode_of(g);
+            const bool pair = mode == ROWS;
+            const int copies = copies_of(g.rows), step = mode == STEPS ? 2 : 1, mine = mode == STEPS ? s : 0;       // this stream's steps
             const int r = pair ? row + s * TILE_ROWS : row & (TILE_ROWS / copies - 1);       // row of the group
+            const int head = g.head + (mode == HEADS ? s : 0);
             const int col = row / (TILE_ROWS / copies) * (STEP / copies);    // the first of a step's tokens that this copy of the row takes
             const bool live = r - lane < g.rows;                 // the warp has rows
             const bool there = r < g.rows;
-            int lo = 0, hi = 0;                                  // tiles without masks
-            if (a.tree) hi = g.axis.n_sink / BN;
+            int lo = 0, hi = 0;                                  // steps without masks
+            if (a.tree) hi = g.axis.n_sink / STEP;
             else hx_whole_tiles(g.axis, g.len - g.nq + (g.r0 + (pair ? s * TILE_ROWS : 0)) / a.group,
-                                g.len - g.nq + (g.r0 + min(g.rows, (pair ? s + 1 : 1) * TILE_ROWS) - 1) / a.group, a.window, a.sinks, BN, &lo, &hi);
+                                g.len - g.nq + (g.r0 + min(g.rows, (pair ? s + 1 : 1) * TILE_ROWS) - 1) / a.group, a.window, a.sinks, STEP, &lo, &hi);
             lo -= t0; hi -= t0;
+            const View view = view_of(a, g, seg.anc, there ? r : 0);
             float mx = -INFINITY, sum = 0.f;
-            for (int j = pair ? 0 : s; j < nt && go; j += pair ? 1 : 2, ++sn) {
-                const uint32_t* valid = sh.valid[(tiles_seen + j) % VALID_RING];
-#pragma unroll 1
-                for (int h = 0; h < 2; ++h) {
-                    if (!(go = warp_wait(smem_at(&sh.s_full[s][h]), sn & 1, quit))) break;
-                    tc_after();
-                    const uint2 v2 = *reinterpret_cast<const uint2*>(valid + 2 * h);
-                    const bool all = (v2.x & v2.y) == 0xffffffffu, whole = j >= lo && j < hi && all;
-                    if (!all) {
-                        // rows that are no entry of the axis (behind the end of a page's use) hold anything, and 0 x NaN is NaN
-                        const int at = kvn + value_place(pair, nt, j), slot = at % NS;
-                        if (!(go = warp_wait(smem_at(&sh.full[slot]), (at / NS) & 1, quit))) break;
-                        if ((row >> 6) == h && !((valid[row >> 5] >> lane) & 1)) {
-                            char* tile = kv_s + slot * S::TILE;
+            for (int i = mine; i < nt; i += step, ++sn) {
+                const int b = sn & 1;
+                if (!(go = warp_wait(smem_at(&sh.s_full[s][b]), (sn >> 1) & 1, quit))) break;
+                tc_after();
+                const uint2 valid = *reinterpret_cast<const uint2*>(sh.valid[mode == HEADS ? s : 0][(before + i) % VALID_RING]);
+                const bool all = (valid.x & valid.y) == 0xffffffffu, whole = i >= lo && i < hi && all;
+                if (!all) {
+                    // rows that are no entry of the axis (behind the end of a page's use) hold anything, and 0 x NaN is NaN
+                    const int at = kvn + value_place(mode, nt, i, s), slot = at % NS;
+                    if (!(go = warp_wait(smem_at(&sh.full[slot]), (at / NS) & 1, quit))) break;
+                    if (!(((row & 32 ? valid.y : valid.x) >> lane) & 1)) {           // two threads to a row of values
+                        char* slot_at = kv_s + slot * S::SLOT;
 #pragma unroll
-                            for (int c = 0; c < S::CHUNKS; ++c) *reinterpret_cast<uint4*>(tile + piece(row, c)) = make_uint4(0, 0, 0, 0);
-                            fence_async();
-                        }
+                        for (int c = 0; c < S::CHUNKS / 2; ++c) *reinterpret_cast<uint4*>(slot_at + piece(row & 63, (row >> 6) * (S::CHUNKS / 2) + c, 64)) = make_uint4(0, 0, 0, 0);
+                        fence_async();
                     }
-                    if (live) {
-                        const bool first = j < (pair ? 1 : 2) && h == 0;
-                        uint64_t seen = 0;
-                        if (!whole) {
-                            uint32_t m[2] = {0, 0};
-                            if (there) sees<2>(a, g, seg.anc, r, (t0 + j) * BN + h * STEP, m);
-                            seen = ((uint64_t)(m[1] & v2.y) << 32 | (m[0] & v2.x)) >> col;
-                        }
-                        // the products of the step before may still add to O; those before it have ended, as these scores came after them
-                        auto settle = [&] { if (!warp_wait(smem_at(&sh.pv[s]), (2 * sn + h - 1) & 1, quit)) return false; tc_after(); return true; };
-                        auto step = [&](auto columns) {
-                            constexpr int NC = decltype(columns)::value;
-                            return softmax_step<D, NC, T>(S_at + h * STEP, O_at + s * 128, col, !whole, seen, first, a.scale_log2, mx, sum, settle);
-                        };
-                        go = copies == 1 ? step(Columns<64>()) : copies == 2 ? step(Columns<32>()) : step(Columns<16>());
-                        if (!go) break;
-                    }
-                    tc_before();
-                    __syncwarp();
-                    if (lane == 0) bar_arrive(smem_at(&sh.p_full[s][h]));
                 }
+                if (live) {
+                    uint64_t seen = 0;
+                    if (!whole) {
+                        uint32_t m[2] = {0, 0};
+                        if (there) sees<2>(a.tree, view, (t0 + i) * STEP, m);
+                        seen = ((uint64_t)(m[1] & valid.y) << 32 | (m[0] & valid.x)) >> col;
+                    }
+                    // the products of the step before may still add to O; those before it have ended, as these scores came after them
+                    auto settle = [&] { if (!warp_wait(smem_at(&sh.pv[s]), (sn - 1) & 1, quit)) return false; tc_after(); return true; };
+                    auto one = [&](auto columns) {
+                        constexpr int NC = decltype(columns)::value;
+                        return softmax_step<D, NC, T>(S_at + b * STEP, O_at + s * 128, col, !whole, seen, i == mine, a.scale_log2, mx, sum, settle);
+                    };
+                    if (!(go = copies == 1 ? one(Columns<64>()) : copies == 2 ? one(Columns<32>()) : one(Columns<16>()))) break;
+                }
+                tc_before();
+                __syncwarp();
+                if (lane == 0) bar_arrive(smem_at(&sh.p_full[s][b]));
             }
             if (!go) break;
 
             // ---- end of the group, or of this block's part of it
-            const bool both = !pair && nt > 1;           // the second stream has half of the tiles of the same rows
+            const bool both = mode == STEPS && nt > 1;   // the second stream has half of the steps of the same rows
             if (a.tree && there) {
                 const uint4 m = seg.anc[(g.r0 + r) / a.group];
                 if (!(m.x | m.y | m.z | m.w)) { mx = -INFINITY; sum = 0.f; }
             }
-            if (pair || s == 0 || both) { if (!(go = warp_wait(smem_at(&sh.o_full[s]), on++ & 1, quit))) break; }
+            if (mode != STEPS || s == 0 || both) { if (!(go = warp_wait(smem_at(&sh.o_full[s]), on++ & 1, quit))) break; }
             if (both && s == 1) {
-                sh.stat[row] = make_float2(mx, sum);
+                sh.stat[1][row] = make_float2(mx, sum);
                 __syncwarp();
                 if (lane == 0) bar_arrive(smem_at(&sh.x_ready));
                 if (!(go = warp_wait(smem_at(&sh.x_free), xn & 1, quit))) break;
                 ++xn;
-            } else if (pair || s == 0) {
+            } else if (mode != STEPS || s == 0) {
                 float f0 = 1.f, f1 = 0.f;
                 if (both) {
                     if (!(go = warp_wait(smem_at(&sh.x_ready), xn & 1, quit))) break;
                     ++xn;
-                    const float2 o = sh.stat[row];
+                    const float2 o = sh.stat[1][row];
                     const float m = fmaxf(mx, o.x), safe = m == -INFINITY ? 0.f : m;
                     f0 = exp2_fast(mx - safe); f1 = exp2_fast(o.x - safe);
                     sum = __fmaf_rn(sum, f0, o.y * f1); mx = m;
                 }
                 tc_after();
-                const bool complete = t0 == 0 && seg.t1 == g.tiles;
+                const bool complete = t0 == 0 && seg.t1 == g.steps;
                 float finite = 0.f;                      // NaN when something of a row's result is not finite
+                float* part = a.part + ((int64_t)blockIdx.x * 2 + (t0 > 0 ? 0 : 1)) * GROUP_ROWS * (D + 2)      // [column][row]; then maxima, sums
+                            + (mode == HEADS ? s * TILE_ROWS : 0);
                 if (copies == 1) {
                     const bool none = sum == 0.f;        // sees nothing here: what the products left says nothing
                     const float inv = none ? 0.f : 1.f / sum;
-                    const Place at = place_of(a, g, r);
-                    float* part = a.part + (((int64_t)blockIdx.x * 2 + (t0 > 0 ? 0 : 1)) * GROUP_ROWS + r) * (D + 4);
+                    const Place at = place_of(a, g, head, there ? r : 0);
                     if (live) {
-#pragma unroll
+                        // through shared memory, so that four lanes write 64 bytes of a row
+                        char* stage = reinterpret_cast<char*>(sh.buf) + warp * 2048;
+#pragma unroll 1
                         for (int c = 0; c < D; c += 32) {
                             uint32_t o[32], p[32];
                             tc_ld32(o, O_at + s * 128 + c);
@@ -849,89 +879,115 @@ __global__ void __launch_bounds__(THREADS, 1) hx_attend_kernel(const AttendArgs 
                                 finite = __fmaf_rn(x, 0.f, finite);
                                 o[i] = __float_as_uint(x);
                             }
-                            if (there && complete) {
+                            if (complete) {
                                 uint32_t w[16];
 #pragma unroll
                                 for (int i = 0; i < 16; ++i) w[i] = Elem<T>::pack(__uint_as_float(o[2 * i]) * inv, __uint_as_float(o[2 * i + 1]) * inv);
-                                T* out = reinterpret_cast<T*>(a.out) + at.out + c;
                                 if (a.out16) {
 #pragma unroll
-                                    for (int i = 0; i < 4; ++i) reinterpret_cast<uint4*>(out)[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
-                                } else {
+                                    for (int i = 0; i < 4; ++i)
+                                        *reinterpret_cast<uint4*>(stage + lane * 64 + ((i ^ ((lane >> 1) & 3)) << 4)) = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+                                    __syncwarp();
 #pragma unroll
-                                    for (int i = 0; i < 16; ++i) reinterpret_cast<uint32_t*>(out)[i] = w[i];
+                                    for (int i = 0; i < 4; ++i) {
+                                        const int q = i * 8 + (lane >> 2), k = lane & 3;
+                                        const uint4 x = *reinterpret_cast<const uint4*>(stage + q * 64 + ((k ^ ((q >> 1) & 3)) << 4));
+                                        const int64_t to = __shfl_sync(0xffffffffu, at.out, q);
+                                        if (r - lane + q < g.rows) *reinterpret_cast<uint4*>(reinterpret_cast<T*>(a.out) + to + c + 8 * k) = x;
+                                    }
+                                    __syncwarp();
+                                } else if (there) {
+#pragma unroll
+                                    for (int i = 0; i < 16; ++i) reinterpret_cast<uint32_t*>(reinterpret_cast<T*>(a.out) + at.out + c)[i] = w[i];
                                 }
                             } else if (there) {
 #pragma unroll
-                                for (int i = 0; i < 8; ++i) reinterpret_cast<uint4*>(part + 4 + c)[i] = make_uint4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+                                for (int i = 0; i < 32; ++i) part[(c + i) * GROUP_ROWS + r] = __uint_as_float(o[i]);
                             }
                         }
                         if (there) {
-                            if (!complete) *reinterpret_cast<float2*>(part) = make_float2(mx, sum);
+                            if (!complete) { part[D * GROUP_ROWS + r] = mx; part[(D + 1) * GROUP_ROWS + r] = sum; }
                             else if (a.lse) a.lse[at.lse] = none ? -INFINITY : __fmaf_rn(mx, LN2, logf(sum));
                         }
                     }
                     if (!there) finite = 0.f;
                 } else {
-                    // the copies of a row joined through shared memory, 16 columns at a time; then thread t writes columns
-                    // 16 / copies * (t % copies) .. of row t / copies
-                    const int room = TILE_ROWS / copies;
+                    // the copies of a row joined through shared memory, as many columns at a time as fit
                     auto together = [&] {
                         __syncwarp();
-                        if (lane == 0) bar_arrive(smem_at(&sh.join));
-                        return warp_wait(smem_at(&sh.join), jn++ & 1, quit);
+                        if (lane == 0) bar_arrive(smem_at(&sh.join[s]));
+                        return warp_wait(smem_at(&sh.join[s]), jn++ & 1, quit);
                     };
-                    sh.stat[row] = make_float2(mx, sum);
+                    const int room = TILE_ROWS / copies, lanes = copies * g.rows;
+                    int width = D;                       // of D, half of it, ... those that the first stream's share of the buffer holds
+                    while (lanes * width > 4 * 512) width = width == 96 ? 32 : width / 2;
+                    const int twist = width < 32 ? 15 : 31;      // columns are permuted by copy and row, so that banks differ
+                    sh.stat[s][row] = make_float2(mx, sum);
                     if (!(go = together())) break;
-                    const int rr = row / copies;
-                    float m = -INFINITY, m2 = -INFINITY, l2 = 0.f;       // of the row at hand, and of the one written
-                    for (int k = 0; k < copies; ++k) { m = fmaxf(m, sh.stat[r + k * room].x); m2 = fmaxf(m2, sh.stat[rr + k * room].x); }
-                    const float safe2 = m2 == -INFINITY ? 0.f : m2;
-                    for (int k = 0; k < copies; ++k) l2 = __fmaf_rn(sh.stat[rr + k * room].y, exp2_fast(sh.stat[rr + k * room].x - safe2), l2);
-                    const float f = sum == 0.f ? 0.f : exp2_fast(mx - (m == -INFINITY ? 0.f : m));
+                    float m = -INFINITY, l = 0.f;        // of the row, over its copies
+                    for (int k = 0; k < copies; ++k) m = fmaxf(m, sh.stat[s][r + k * room].x);
+                    const float safe = m == -INFINITY ? 0.f : m;
+                    for (int k = 0; k < copies; ++k) l = __fmaf_rn(sh.stat[s][r + k * room].y, exp2_fast(sh.stat[s][r + k * room].x - safe), l);
+                    const float f = sum == 0.f ? 0.f : exp2_fast(mx - safe);
                     f0 *= f; f1 *= f;
-                    const bool none = l2 == 0.f, write = rr < g.rows;
-                    const float inv = none ? 0.f : 1.f / l2;
-                    const Place at = place_of(a, g, write ? rr : 0);
-                    float* part = a.part + (((int64_t)blockIdx.x * 2 + (t0 > 0 ? 0 : 1)) * GROUP_ROWS + rr) * (D + 4);
-                    for (int c = 0; c < D; c += 16) {
-                        uint32_t o[16], p[16];
-                        float* buf = sh.buf[(c >> 4) & 1];
-                        tc_ld16(o, O_at + c);
-                        if (both) tc_ld16(p, O_at + 128 + c);
-                        tc_ld_wait();
+                    if (row < room && there) {
+                        sh.fin[s][r] = l == 0.f ? 0.f : complete ? 1.f / l : 1.f;
+                        const Place at = place_of(a, g, head, r);
+                        if (!complete) { part[D * GROUP_ROWS + r] = m; part[(D + 1) * GROUP_ROWS + r] = l; }
+                        else if (a.lse) a.lse[at.lse] = l == 0.f ? -INFINITY : __fmaf_rn(m, LN2, logf(l));
+                    }
+                    const int at_row = row / room * g.rows + r;
+                    float *buf = sh.buf + s * 4 * 512, *put = buf + at_row * width;
+                    for (int c0 = 0; c0 < D; c0 += width) {
+#pragma unroll 1
+                        for (int c = 0; c < width && live; c += 16) {
+                            uint32_t o[16], p[16];
+                            tc_ld16(o, O_at + s * 128 + c0 + c);
+                            if (both) tc_ld16(p, O_at + 128 + c0 + c);
+                            tc_ld_wait();
+                            if (there) {
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            float x = f0 == 0.f ? 0.f : __uint_as_float(o[i]) * f0;
-                            if (both && f1 != 0.f) x += __uint_as_float(p[i]) * f1;
-                            buf[row * 17 + i] = x;
+                                for (int i = 0; i < 16; ++i) {
+                                    float x = f0 == 0.f ? 0.f : __uint_as_float(o[i]) * f0;
+                                    if (both && f1 != 0.f) x += __uint_as_float(p[i]) * f1;
+                                    put[(c + i) ^ (at_row & twist)] = x;
+                                }
+                            }
+                        }
+                        if (both && c0 + width >= D) {   // the second stream's sums are read
+                            tc_before();
+                            __syncwarp();
+                            if (lane == 0) bar_arrive(smem_at(&sh.x_free));
                         }
                         if (!(go = together())) break;
-                        for (int i = (row % copies) * (16 / copies); i < (row % copies + 1) * (16 / copies); i += 2) {
+                        const int pairs = width / 2;
+                        for (int e = row; e < g.rows * pairs; e += 128) {
+                            const int q = e / pairs, c = 2 * (e - q * pairs);
                             float x = 0.f, y = 0.f;
-                            for (int k = 0; k < copies; ++k) { x += buf[(rr + k * room) * 17 + i]; y += buf[(rr + k * room) * 17 + i + 1]; }
-                            if (none) x = y = 0.f;
-                            if (!write) continue;
+                            for (int k = 0; k < copies; ++k) {
+                                const int from = k * g.rows + q;
+                                x += buf[from * width + (c ^ (from & twist))];
+                                y += buf[from * width + ((c + 1) ^ (from & twist))];
+                            }
+                            const float inv = sh.fin[s][q];
+                            if (inv == 0.f) x = y = 0.f;
                             finite = __fmaf_rn(x, 0.f, __fmaf_rn(y, 0.f, finite));
-                            if (complete) *reinterpret_cast<uint32_t*>(reinterpret_cast<T*>(a.out) + at.out + c + i) = Elem<T>::pack(x * inv, y * inv);
-                            else *reinterpret_cast<float2*>(part + 4 + c + i) = make_float2(x, y);
+                            if (complete) *reinterpret_cast<uint32_t*>(reinterpret_cast<T*>(a.out) + place_of(a, g, head, q).out + c0 + c) = Elem<T>::pack(x * inv, y * inv);
+                            else { part[(c0 + c) * GROUP_ROWS + q] = x; part[(c0 + c + 1) * GROUP_ROWS + q] = y; }
                         }
+                        if (!(go = together())) break;
                     }
                     if (!go) break;
-                    if (write && row % copies == 0) {
-                        if (!complete) *reinterpret_cast<float2*>(part) = make_float2(m2, l2);
-                        else if (a.lse) a.lse[at.lse] = none ? -INFINITY : __fmaf_rn(m2, LN2, logf(l2));
-                    }
                 }
                 odd = odd || finite != 0.f;
                 tc_before();
                 __syncwarp();
-                if (both && lane == 0) bar_arrive(smem_at(&sh.x_free));
+                if (both && copies == 1 && lane == 0) bar_arrive(smem_at(&sh.x_free));
             }
             __syncwarp();
             if (lane == 0) bar_arrive(smem_at(&sh.seg_empty[si]));
-            kvn += 2 * nt;
-            tiles_seen += nt;
+            kvn += loads_of(mode, nt);
+            before += nt;
         }
         if (__any_sync(0xffffffffu, odd) && lane == 0) reinterpret_cast<volatile int4*>(a.desc)[blockIdx.x].w = 1;
     }
@@ -945,19 +1001,20 @@ __global__ void __launch_bounds__(THREADS, 1) hx_attend_kernel(const AttendArgs 
 
 // One row of a group by one warp, reading what the row sees and nothing else.
 template <int D, class T>
-__device__ void one_row(const AttendArgs& a, const Group& g, const uint4* anc, int r) {
-    const int lane = threadIdx.x & 31, qi = (g.r0 + r) / a.group, head = g.head * a.group + g.r0 + r - qi * a.group;
-    const uint32_t* q = reinterpret_cast<const uint32_t*>(a.q + 2 * ((int64_t)(g.row0 + qi) * a.q_row + (int64_t)head * a.q_head));
+__device__ void one_row(const AttendArgs& a, const Group& g, const uint4* anc, int head, int r) {
+    const int lane = threadIdx.x & 31, qi = (g.r0 + r) / a.group;
+    const uint32_t* q = reinterpret_cast<const uint32_t*>(a.q + 2 * ((int64_t)(g.row0 + qi) * a.q_row + (int64_t)(head * a.group + g.r0 + r - qi * a.group) * a.q_head));
+    const View view = view_of(a, g, anc, r);
     float m = -INFINITY, l = 0.f, acc[D / 32];
 #pragma unroll
     for (int i = 0; i < D / 32; ++i) acc[i] = 0.f;
     for (int x0 = 0; x0 < g.axis.n; x0 += 32) {
         uint32_t bits[1];
-        sees<1>(a, g, anc, r, x0, bits);
+        sees<1>(a.tree, view, x0, bits);
         bool drafted;
         const int at = row_of(a, g, x0 + lane, &drafted);
         const bool see = at >= 0 && ((bits[0] >> lane) & 1);
-        const int64_t byte = (int64_t)at * (drafted ? a.draft_row_bytes : (int64_t)a.token_bytes) + (int64_t)g.head * (D * 2);
+        const int64_t byte = (int64_t)at * (drafted ? a.draft_row_bytes : (int64_t)a.token_bytes) + (int64_t)head * (D * 2);
         const char *k = (drafted ? a.k_draft : a.k) + byte, *v = (drafted ? a.v_draft : a.v) + byte;
         float s = -INFINITY;
         if (see) {
@@ -989,10 +1046,11 @@ __device__ void one_row(const AttendArgs& a, const Group& g, const uint4* anc, i
         }
     }
     const float inv = l == 0.f ? 0.f : 1.f / l;
-    T* out = reinterpret_cast<T*>(a.out) + (int64_t)(g.row0 + qi) * a.o_row + (int64_t)head * a.o_head;
+    const Place at = place_of(a, g, head, r);
+    T* out = reinterpret_cast<T*>(a.out) + at.out;
 #pragma unroll
     for (int i = 0; i < D / 32; ++i) out[i * 32 + lane] = T(l == 0.f ? 0.f : acc[i] * inv);
-    if (a.lse && lane == 0) a.lse[(int64_t)(g.row0 + qi) * a.n_kv_heads * a.group + head] = l == 0.f ? -INFINITY : __fmaf_rn(m, LN2, logf(l));
+    if (a.lse && lane == 0) a.lse[at.lse] = l == 0.f ? -INFINITY : __fmaf_rn(m, LN2, logf(l));
 }
 
 constexpr int JOIN_THREADS = 256;
@@ -1018,39 +1076,38 @@ __global__ void __launch_bounds__(JOIN_THREADS) hx_attend_join_kernel(const Atte
             __syncthreads();
             if (a.tree && tid < 32) ancestors(a, g.item / a.row_tiles, anc, link);
             __syncthreads();
-            for (int r = tid >> 5; r < g.rows; r += JOIN_THREADS / 32) one_row<D, T>(a, g, anc, r);
+            for (int r = tid >> 5; r < g.rows * g.heads; r += JOIN_THREADS / 32) one_row<D, T>(a, g, anc, g.head + r / g.rows, r % g.rows);
         }
     }
     if (de.x == 0) return;
     for (int i = 0; i < de.x; ++i) if (a.desc[blockIdx.x + i].w) return;     // that block has computed the group whole
     const Group g = group_of(a, de.y, de.z);
-    constexpr int PER = D / 4;                           // four elements to a thread
-    for (int e = tid; e < g.rows * PER; e += JOIN_THREADS) {
-        const int r = e / PER, c = (e - r * PER) * 4;
-        float m = -INFINITY, l = 0.f;
-        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    constexpr int PER = D / 4;                           // four elements to a thread, rows along the threads
+    const int rows = g.rows * g.heads;
+    for (int e = tid; e < rows * PER; e += JOIN_THREADS) {
+        const int c = e / rows * 4, hr = e - e / rows * rows, head = g.head + hr / g.rows, r = hr % g.rows;
+        float m = -INFINITY, l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
         for (int i = 0; i < de.x; ++i) {
-            const float* p = a.part + (((int64_t)(blockIdx.x + i) * 2 + (i ? 0 : 1)) * GROUP_ROWS + r) * (D + 4);
-            const float2 st = *reinterpret_cast<const float2*>(p);
-            const float mn = fmaxf(m, st.x), safe = mn == -INFINITY ? 0.f : mn, fo = exp2_fast(m - safe), fn = exp2_fast(st.x - safe);
-            const float4 x = *reinterpret_cast<const float4*>(p + 4 + c);
-            l = __fmaf_rn(l, fo, st.y * fn);
-            o.x = __fmaf_rn(o.x, fo, x.x * fn); o.y = __fmaf_rn(o.y, fo, x.y * fn);
-            o.z = __fmaf_rn(o.z, fo, x.z * fn); o.w = __fmaf_rn(o.w, fo, x.w * fn);
+            const float* p = a.part + ((int64_t)(blockIdx.x + i) * 2 + (i ? 0 : 1)) * GROUP_ROWS * (D + 2) + (head - g.head) * TILE_ROWS + r;
+            const float pm = p[D * GROUP_ROWS], pl = p[(D + 1) * GROUP_ROWS];
+            const float mn = fmaxf(m, pm), safe = mn == -INFINITY ? 0.f : mn, fo = exp2_fast(m - safe), fn = exp2_fast(pm - safe);
+            l = __fmaf_rn(l, fo, pl * fn);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) o[k] = __fmaf_rn(o[k], fo, p[(c + k) * GROUP_ROWS] * fn);
             m = mn;
         }
-        const int qi = (g.r0 + r) / a.group, head = g.head * a.group + g.r0 + r - qi * a.group;
+        const Place at = place_of(a, g, head, r);
         const float inv = l == 0.f ? 0.f : 1.f / l;
-        uint32_t* to = reinterpret_cast<uint32_t*>(reinterpret_cast<T*>(a.out) + (int64_t)(g.row0 + qi) * a.o_row + (int64_t)head * a.o_head + c);
-        to[0] = Elem<T>::pack(o.x * inv, o.y * inv);
-        to[1] = Elem<T>::pack(o.z * inv, o.w * inv);
-        if (c == 0 && a.lse) a.lse[(int64_t)(g.row0 + qi) * a.n_kv_heads * a.group + head] = l == 0.f ? -INFINITY : __fmaf_rn(m, LN2, logf(l));
+        uint32_t* to = reinterpret_cast<uint32_t*>(reinterpret_cast<T*>(a.out) + at.out + c);
+        to[0] = Elem<T>::pack(o[0] * inv, o[1] * inv);
+        to[1] = Elem<T>::pack(o[2] * inv, o[3] * inv);
+        if (c == 0 && a.lse) a.lse[at.lse] = l == 0.f ? -INFINITY : __fmaf_rn(m, LN2, logf(l));
     }
 }
 
 constexpr int MAX_BLOCKS = 148;      // one to each multiprocessor
 
-size_t part_bytes(int D) { return (size_t)MAX_BLOCKS * 2 * GROUP_ROWS * (D + 4) * sizeof(float); }
+size_t part_bytes(int D) { return (size_t)MAX_BLOCKS * 2 * GROUP_ROWS * (D + 2) * sizeof(float); }
 
 typedef CUresult (*EncodeTiled)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*, const cuuint32_t*,
                                 CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
@@ -1143,7 +1200,7 @@ AttendArgs args_of(const HxCore& core, const hx_kv_cache* c, int layer, const hx
     AttendArgs a{};
     a.k = static_cast<const char*>(c->k) + layer * c->layer_stride * 2;
     a.v = static_cast<const char*>(c->v) + layer * c->layer_stride * 2;
-    a.chunk = hx_power_in(c->page_tokens, BN);
+    a.chunk = hx_power_in(c->page_tokens, STEP);
     a.page_rows = (int)(c->page_stride / ((int64_t)c->n_kv_heads * c->head_dim));
     a.token_bytes = c->n_kv_heads * c->head_dim * 2;
     a.page_tokens = c->page_tokens; a.n_pages = c->n_pages; a.max_seqs = c->max_seqs; a.max_pages = c->max_pages; a.n_kv_heads = c->n_kv_heads;
