@@ -51,7 +51,7 @@ constexpr int SEGS = 2;              // groups looked up ahead
 constexpr int VALID_RING = 16;
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 constexpr float GROWTH = 8.f;        // powers of two that the maximum may grow before O is rescaled
-constexpr unsigned long long WAIT_NS = 2000000000ull;    // a wait that lasts this long ends the kernel with HX_ERR_TIMEOUT
+constexpr long long WAIT_CYCLES = 4000000000ll;          // a wait that lasts this long (some two seconds) ends the kernel with HX_ERR_TIMEOUT
 
 struct AttendArgs {
     // cache
@@ -71,7 +71,7 @@ struct AttendArgs {
     int n, max_q, row_tiles;         // groups of a sequence and head: ceil(max_q * G / 256)
     int window, sinks;
     const char *k_draft, *v_draft; int64_t draft_row_bytes;
-    int tree, planned, out16;        // planned: shares of the line of steps; else whole groups in turn; out16: 16-byte stores
+    int tree, planned, out16, twin;       // planned: shares of the line of steps; else whole groups in turn; out16: 16-byte stores; twin: small groups two heads at a time
     // partial results
     float* part; int4* desc;
     int* status;
@@ -113,16 +113,16 @@ __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
     asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.b32 %0, 1, 0, p;\n}" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
     return ok != 0;
 }
-__device__ __forceinline__ unsigned long long now_ns() { unsigned long long t; asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t)); return t; }
-// False when the block is to end: this wait or another has lasted too long.
+// False when the block is to end: this wait or another has lasted too long.  (The clock of the multiprocessor: reading the global
+// timer takes as long as a step.)
 __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile int* quit) {
     if (bar_try(bar, parity)) return true;
-    const unsigned long long t0 = now_ns();
+    const long long since = clock64();
     for (uint32_t i = 1;; ++i) {
         if (bar_try(bar, parity)) return true;
         if ((i & 63) == 0) {
             if (*quit) return false;
-            if (now_ns() - t0 > WAIT_NS) { *quit = 1; return false; }
+            if (clock64() - since > WAIT_CYCLES) { *quit = 1; return false; }
         }
     }
 }
@@ -217,7 +217,7 @@ __device__ __forceinline__ Group group_of(const AttendArgs& a, int item, int hea
     g.r0 = (item - b * a.row_tiles) * GROUP_ROWS;
     if (!request(a, b, &g.seq, &g.row0, &g.nq, &g.len) && report && g.r0 == 0 && head == 0) atomicExch(a.status, HX_ERR_INVALID_ARG);
     g.rows = min(GROUP_ROWS, g.nq * a.group - g.r0);
-    g.heads = g.rows <= TILE_ROWS && head + 1 < a.n_kv_heads ? 2 : 1;
+    g.heads = a.twin && g.rows <= TILE_ROWS && head + 1 < a.n_kv_heads ? 2 : 1;
     g.axis.n_sink = g.axis.gap = g.axis.n = 0;
     if (g.rows <= 0) { g.rows = 0; return g; }
     if (a.tree) { g.axis.n_sink = hx_round_up(g.len, max(a.chunk, 4)); g.axis.n = g.axis.n_sink + g.nq; }
@@ -227,10 +227,10 @@ __device__ __forceinline__ Group group_of(const AttendArgs& a, int item, int hea
 }
 
 // Steps over the KV heads of an item: of its groups, or pairs of groups.
-__device__ __forceinline__ int head_steps(const AttendArgs& a, int rows) { return rows > TILE_ROWS ? a.n_kv_heads : (a.n_kv_heads + 1) / 2; }
+__device__ __forceinline__ int head_steps(const AttendArgs& a, int rows) { return rows > TILE_ROWS || !a.twin ? a.n_kv_heads : (a.n_kv_heads + 1) / 2; }
 
 // The line of steps: prefix[i] = units before item i.
-__device__ __forceinline__ int step_cost(const AttendArgs& a, int rows) { return rows > TILE_ROWS || a.n_kv_heads > 1 ? BOTH_COST : ALTERNATE_COST; }
+__device__ __forceinline__ int step_cost(const AttendArgs& a, int rows) { return rows > TILE_ROWS || (a.twin && a.n_kv_heads > 1) ? BOTH_COST : ALTERNATE_COST; }
 struct Plan { int64_t total; int shares; };
 __device__ Plan make_plan(const AttendArgs& a, int64_t* prefix, int64_t* scan, int n_blocks, bool report) {
     const int tid = threadIdx.x, nt = blockDim.x, lane = tid & 31, warp = tid >> 5, items = a.n * a.row_tiles;
@@ -282,7 +282,7 @@ __device__ __forceinline__ bool next_group(const AttendArgs& a, const int64_t* p
             *g = group_of(a, (int)(w.unit / a.n_kv_heads), head, true);
             w.unit += w.step;
             *t0 = 0; *t1 = g->steps; *start = 0;
-            if (g->steps && (g->rows > TILE_ROWS || head % 2 == 0)) return true;
+            if (g->steps && (g->rows > TILE_ROWS || !a.twin || head % 2 == 0)) return true;
             continue;
         }
         const int64_t u = w.unit;
@@ -294,7 +294,7 @@ __device__ __forceinline__ bool next_group(const AttendArgs& a, const int64_t* p
         const int at = (int)(in / units);
         const int64_t x = in - at * units, left = min(units - x, w.end - u);
         w.unit = u + left;
-        if (at) *g = group_of(a, lo, g->rows > TILE_ROWS ? at : 2 * at);
+        if (at) *g = group_of(a, lo, g->rows > TILE_ROWS || !a.twin ? at : 2 * at);
         const int cost = step_cost(a, g->rows);             // step i belongs to the share of unit GROUP_COST + i * cost
         *t0 = (int)((max((int64_t)0, x - GROUP_COST) + cost - 1) / cost);
         *t1 = min((int)((max((int64_t)0, x + left - GROUP_COST) + cost - 1) / cost), g->steps);
@@ -432,7 +432,7 @@ struct Shared {
     alignas(16) float buf[8 * 512];  // results on their way out, 2 KB to a warp; a stream's four also join the copies of rows
     float fin[2][TILE_ROWS / 2];     // what the rows' sums are multiplied by
     int link[HX_TREE_MAX];
-    unsigned long long full[16], empty[16], q_full, q_empty, s_full[2][2], p_full[2][2], pv[2], o_full[2], x_ready, x_free, join[2], seg_full[SEGS], seg_empty[SEGS], drained[2];
+    unsigned long long full[16], empty[16], q_full, q_empty, s_full[2][2], p_full[2][2], pv[2], o_full[2], x_ready, x_free, join[2], group_done[2], seg_full[SEGS], seg_empty[SEGS], drained[2];
     uint32_t tmem;
     int quit;
 };
@@ -440,27 +440,31 @@ struct Shared {
 // How a group is shared by the streams: 128 rows each of the same head, the same rows of two heads, or alternate steps of one.
 enum Mode { ROWS, HEADS, STEPS };
 __device__ __forceinline__ Mode mode_of(const Group& g) { return g.rows > TILE_ROWS ? ROWS : g.heads == 2 ? HEADS : STEPS; }
-// Loads of a group come in the order in which the products need them: the keys of the first `lead` steps (two to a stream), then values
-// of a step and keys of the step `lead` ahead, in turn; of two heads, one behind the other.  Places of step i's for stream s among n:
-__device__ __forceinline__ int lead_of(Mode m) { return m == STEPS ? 4 : 2; }
-__device__ __forceinline__ int loads_of(Mode m, int n) { return m == HEADS ? 4 * n : 2 * n; }
+// Loads of a group come in the order in which a stream needs them: the keys of its first two steps, then values of a step and keys
+// of the one two ahead, in turn.  Streams that read the same rows share them; otherwise each has every second load, and so the same
+// slots throughout a group: a wait can tell a slot's use from the one before it only, and the use before may not be another stream's,
+// which this one does not see come.  (For the same reason the streams wait for one another between groups.)
+// A group has `rounds` of steps; in alternate steps the last round may lack the second one: its places stay empty.
+__device__ __forceinline__ int rounds_of(Mode m, int n) { return m == STEPS ? (n + 1) / 2 : n; }
+__device__ __forceinline__ int loads_of(Mode m, int n) { return m == ROWS ? 2 * n : 4 * rounds_of(m, n); }
 __device__ __forceinline__ int key_place(Mode m, int i, int s) {
-    const int at = i < lead_of(m) ? i : 2 * i - lead_of(m) + 1;
-    return m == HEADS ? 2 * at + s : at;
+    const int at = i < 2 ? i : 2 * i - 1;
+    return m == ROWS ? at : 2 * at + s;
 }
-__device__ __forceinline__ int value_place(Mode m, int n, int i, int s) {
-    const int at = min(n, lead_of(m) + i) + i;
-    return m == HEADS ? 2 * at + s : at;
+__device__ __forceinline__ int value_place(Mode m, int rounds, int i, int s) {
+    const int at = min(rounds, i + 2) + i;
+    return m == ROWS ? at : 2 * at + s;
 }
-
-struct Load { bool keys; int step, head; };
-// Load number o of a group of n steps.
+struct Load { bool keys; int step, head, stream; };
+// Load number o of a group of n steps; its step is n or more where the place stays empty.
 __device__ __forceinline__ Load load_at(Mode m, int n, int o) {
     Load l;
-    l.head = m == HEADS ? o & 1 : 0;
-    const int at = m == HEADS ? o >> 1 : o, lead = min(lead_of(m), n), q = at - lead, turns = 2 * (n - lead);
+    l.stream = m == ROWS ? 0 : o & 1;
+    l.head = m == HEADS ? l.stream : 0;
+    const int rounds = rounds_of(m, n), at = m == ROWS ? o : o >> 1, lead = min(2, rounds), q = at - lead, turns = 2 * (rounds - lead);
     l.keys = q < 0 || (q < turns && (q & 1));
-    l.step = q < 0 ? at : q < turns ? (q >> 1) + (q & 1 ? lead : 0) : q - (n - lead);
+    const int i = q < 0 ? at : q < turns ? (q >> 1) + (q & 1 ? lead : 0) : q - (rounds - lead);
+    l.step = m == STEPS ? 2 * i + l.stream : i;
     return l;
 }
 
@@ -562,7 +566,7 @@ __global__ void __launch_bounds__(THREADS, 1) hx_attend_kernel(const AttendArgs 
         bar_init(smem_at(&sh.q_full), 32); bar_init(smem_at(&sh.q_empty), 2);
         for (int i = 0; i < 2; ++i) {
             for (int h = 0; h < 2; ++h) { bar_init(smem_at(&sh.s_full[i][h]), 1); bar_init(smem_at(&sh.p_full[i][h]), 4); }
-            bar_init(smem_at(&sh.pv[i]), 1); bar_init(smem_at(&sh.o_full[i]), 1);
+            bar_init(smem_at(&sh.pv[i]), 1); bar_init(smem_at(&sh.o_full[i]), 1); bar_init(smem_at(&sh.group_done[i]), 1);
         }
         bar_init(smem_at(&sh.x_ready), 4); bar_init(smem_at(&sh.x_free), 4); bar_init(smem_at(&sh.join[0]), 4); bar_init(smem_at(&sh.join[1]), 4);
         for (int i = 0; i < SEGS; ++i) { bar_init(smem_at(&sh.seg_full[i]), 1); bar_init(smem_at(&sh.seg_empty[i]), LOADERS + 2 + 8); }
@@ -613,10 +617,10 @@ __global__ void __launch_bounds__(THREADS, 1) hx_attend_kernel(const AttendArgs 
                 uint32_t bits = 0;                       // of the lane's four entries
                 if (a.chunk < 4) {
                     bool d;
-                    if (mine) { rows.x = row_of(a, g, x, &d); rows.y = row_of(a, g, x + 1, &d); rows.z = row_of(a, g, x + 2, &d); rows.w = row_of(a, g, x + 3, &d); }
+                    if (mine && i < nt) { rows.x = row_of(a, g, x, &d); rows.y = row_of(a, g, x + 1, &d); rows.z = row_of(a, g, x + 2, &d); rows.w = row_of(a, g, x + 3, &d); }
                     bits = (uint32_t)(rows.x >= 0) | (uint32_t)(rows.y >= 0) << 1 | (uint32_t)(rows.z >= 0) << 2 | (uint32_t)(rows.w >= 0) << 3;
                 } else {
-                    int n_have = mine ? max(0, min(per, (a.tree && !drafted ? g.len : g.axis.n) - x)) : 0;       // rows of the chunk that are entries of the axis
+                    int n_have = mine && i < nt ? max(0, min(per, (a.tree && !drafted ? g.len : g.axis.n) - x)) : 0;       // rows of the chunk that are entries of the axis
                     if (drafted) rows.x = g.row0 + x - g.axis.n_sink;
                     else if (n_have > 0 && page >= 0 && page < a.n_pages) rows.x = page * a.page_rows + (a.tree ? x : hx_axis_pos(g.axis, x)) % a.page_tokens;
                     else if (n_have > 0) { n_have = 0; atomicExch(a.status, HX_ERR_INVALID_ARG); }
@@ -626,6 +630,10 @@ __global__ void __launch_bounds__(THREADS, 1) hx_attend_kernel(const AttendArgs 
                 const int at = kvn + o, slot = at % NS;
                 const uint32_t bar = smem_at(&sh.full[slot]), to = smem_at(kv_s + slot * S::SLOT) + lane * per * 128;
                 if (!(go = warp_wait(smem_at(&sh.empty[slot]), ((at / NS) & 1) ^ 1, quit))) break;
+                if (i >= nt) {                           // an empty place
+                    if (lane == 0) bar_arrive(bar);
+                    continue;
+                }
                 if (load.keys) {
                     bits <<= 4 * (lane & 7);
 #pragma unroll
@@ -648,80 +656,87 @@ __global__ void __launch_bounds__(THREADS, 1) hx_attend_kernel(const AttendArgs 
             seen += nt;
         }
         if (!go) {                                       // copies that are on their way end before the block does
-            const unsigned long long since = now_ns();
-            while (now_ns() - since < WAIT_NS / 100) { }
+            const long long since = clock64();
+            while (clock64() - since < WAIT_CYCLES / 100) { }
         }
     } else if (role == 2) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
         if (warp < 10) {
-            // ---- products of one stream
+            // ---- products of one stream: one thread, as every instruction of this loop is on the way from weights to scores
+            if (lane == 0) {
             constexpr uint32_t QK = product(Elem<T>::FORMAT, STEP, false), PV = product(Elem<T>::FORMAT, D, true);
             const int s = warp - 8;
             const uint32_t q_m = matrix(smem_at(q_s), 16), k_m = matrix(smem_at(kv_s), 16), v_m = matrix(smem_at(kv_s), 8192);
-            const uint32_t S_at = uniform(tmem + s * 128), O_at = uniform(tmem + 256 + s * 128);
+            const uint32_t S_at = tmem + s * 128, O_at = tmem + 256 + s * 128;
+            const uint32_t full = smem_at(&sh.full[0]), empty = smem_at(&sh.empty[0]), s_full = smem_at(&sh.s_full[s][0]), p_full = smem_at(&sh.p_full[s][0]);
             int kvn = 0, sn = 0;                         // loads before the group, steps of this stream so far
             bool go = true;
             for (int n = 0; go; ++n) {
                 const int si = n % SEGS;
-                if (!(go = warp_wait(smem_at(&sh.seg_full[si]), (n / SEGS) & 1, quit))) break;
+                if (!(go = bar_wait(smem_at(&sh.seg_full[si]), (n / SEGS) & 1, quit))) break;
                 const int nt = sh.seg[si].t1 - sh.seg[si].t0;
                 const Mode mode = mode_of(sh.seg[si].g);
-                __syncwarp();
-                if (lane == 0) bar_arrive(smem_at(&sh.seg_empty[si]));
+                bar_arrive(smem_at(&sh.seg_empty[si]));
                 if (nt <= 0) break;
-                if (!(go = warp_wait(smem_at(&sh.q_full), n & 1, quit))) break;
-                const uint32_t q_t = uniform(q_m + (mode == STEPS ? 0 : s) * (S::TILE >> 4));
-                const int step = mode == STEPS ? 2 : 1, mine = mode == STEPS ? s : 0;          // this stream's steps: mine, mine + step, ...
-                // a slot, and q, is given back by both streams, or twice by the one that reads it alone
-                auto give_back = [&](uint32_t bar, bool twice) { tc_commit(bar); if (twice) tc_commit(bar); };
-                auto ready = [&](int at) {
-                    if (!warp_wait(smem_at(&sh.full[at % NS]), (at / NS) & 1, quit)) return false;
-                    tc_after();
-                    return true;
-                };
-                // scores of step i, this stream's number k: into buffer k & 1
+                if (!(go = bar_wait(smem_at(&sh.q_full), n & 1, quit))) break;
+                const uint32_t q_t = q_m + (mode == STEPS ? 0 : s) * (S::TILE >> 4);
+                const int rounds = rounds_of(mode, nt), own = mode == STEPS ? (nt + 1 - s) / 2 : nt;         // this stream's steps
+                const bool alone = mode != ROWS;         // a slot that this stream reads alone is given back for the other one too
+                // scores of this stream's step i: number k of all, into buffer k & 1
                 auto scores = [&](int i, int k) {
                     const int at = kvn + key_place(mode, i, s), slot = at % NS;
-                    if (!ready(at)) return false;
-                    const uint32_t k_t = uniform(k_m + slot * (S::SLOT >> 4)), to = uniform(S_at + (k & 1) * STEP);
-                    if (elect()) {
+                    if (!bar_wait(full + slot * 8, (at / NS) & 1, quit)) return false;
+                    tc_after();
+                    const uint32_t k_t = k_m + slot * (S::SLOT >> 4), to = S_at + (k & 1) * STEP;
 #pragma unroll
-                        for (int ks = 0; ks < D / 16; ++ks)
-                            tc_mma_ss(to, q_t + (ks >> 2) * 1024 + (ks & 3) * 2, k_t + (ks >> 2) * 512 + (ks & 3) * 2, QK, ks > 0);
-                        tc_commit(smem_at(&sh.s_full[s][k & 1]));
-                        give_back(smem_at(&sh.empty[slot]), mode != ROWS);
-                        if (i + step >= nt) give_back(smem_at(&sh.q_empty), nt == 1 && mode == STEPS);       // no products after these read q
+                    for (int ks = 0; ks < D / 16; ++ks)
+                        tc_mma_ss(to, q_t + (ks >> 2) * 1024 + (ks & 3) * 2, k_t + (ks >> 2) * 512 + (ks & 3) * 2, QK, ks > 0);
+                    tc_commit(s_full + (k & 1) * 8);
+                    tc_commit(empty + slot * 8);
+                    if (alone) bar_arrive(empty + slot * 8);
+                    if (i + 1 == own) {                  // no products after these read q
+                        tc_commit(smem_at(&sh.q_empty));
+                        if (nt == 1 && mode == STEPS) bar_arrive(smem_at(&sh.q_empty));
                     }
-                    __syncwarp();
                     return true;
                 };
                 // weights of step i, number k, times its values
                 auto values = [&](int i, int k) {
-                    const int at = kvn + value_place(mode, nt, i, s), slot = at % NS;
-                    if (!ready(at) || !warp_wait(smem_at(&sh.p_full[s][k & 1]), (k >> 1) & 1, quit)) return false;
+                    const int at = kvn + value_place(mode, rounds, i, s), slot = at % NS;
+                    if (!bar_wait(full + slot * 8, (at / NS) & 1, quit) || !bar_wait(p_full + (k & 1) * 8, (k >> 1) & 1, quit)) return false;
                     tc_after();
-                    const uint32_t v_t = uniform(v_m + slot * (S::SLOT >> 4)), from = uniform(S_at + (k & 1) * STEP);
-                    if (elect()) {
+                    const uint32_t v_t = v_m + slot * (S::SLOT >> 4), from = S_at + (k & 1) * STEP;
 #pragma unroll
-                        for (int ks = 0; ks < STEP / 16; ++ks) tc_mma_ts(O_at, from + ks * 8, v_t + ks * 128, PV, !(i == mine && ks == 0));
-                        tc_commit(smem_at(&sh.pv[s]));
-                        give_back(smem_at(&sh.empty[slot]), mode != ROWS);
-                        if (i + step >= nt) tc_commit(smem_at(&sh.o_full[s]));
-                    }
-                    __syncwarp();
+                    for (int ks = 0; ks < STEP / 16; ++ks) tc_mma_ts(O_at, from + ks * 8, v_t + ks * 128, PV, !(i == 0 && ks == 0));
+                    tc_commit(smem_at(&sh.pv[s]));
+                    tc_commit(empty + slot * 8);
+                    if (alone) bar_arrive(empty + slot * 8);
+                    if (i + 1 == own) tc_commit(smem_at(&sh.o_full[s]));
                     return true;
                 };
-                for (int k = 0; k < 2 && mine + k * step < nt; ++k) go = go && scores(mine + k * step, sn + k);
-                for (int i = mine; i < nt && go; i += step, ++sn)
-                    go = values(i, sn) && (i + 2 * step >= nt || scores(i + 2 * step, sn + 2));
+                auto skip = [&](int at) {                // an empty place
+                    if (!bar_wait(full + at % NS * 8, (at / NS) & 1, quit)) return false;
+                    bar_arrive(empty + at % NS * 8); bar_arrive(empty + at % NS * 8);
+                    return true;
+                };
+                for (int i = 0; i < min(rounds, 2); ++i) go = go && (i < own ? scores(i, sn + i) : skip(kvn + key_place(mode, i, s)));
+                for (int i = 0; i < rounds && go; ++i) {
+                    go = i < own ? values(i, sn) : skip(kvn + value_place(mode, rounds, i, s));
+                    if (i + 2 < rounds) go = go && (i + 2 < own ? scores(i + 2, sn + 2) : skip(kvn + key_place(mode, i + 2, s)));
+                    sn += i < own;
+                }
+                // the other stream has seen its loads of this group come
+                bar_arrive(smem_at(&sh.group_done[s]));
+                go = go && bar_wait(smem_at(&sh.group_done[1 - s]), n & 1, quit);
                 kvn += loads_of(mode, nt);
             }
             if (!go) {                                   // what was issued ends before the tensor memory is given back
-                if (elect()) tc_commit(smem_at(&sh.drained[s]));
-                __syncwarp();
-                const unsigned long long t0 = now_ns();
-                while (!bar_try(smem_at(&sh.drained[s]), 0) && now_ns() - t0 < WAIT_NS) { }
+                tc_commit(smem_at(&sh.drained[s]));
+                const long long since = clock64();
+                while (!bar_try(smem_at(&sh.drained[s]), 0) && clock64() - since < WAIT_CYCLES) { }
             }
+            }
+            __syncwarp();
         } else if (warp == 10) {
             // ---- groups, and their rows of q
             Walk w = begin_walk(a, plan, blockIdx.x, gridDim.x);
@@ -800,7 +815,7 @@ __global__ void __launch_bounds__(THREADS, 1) hx_attend_kernel(const AttendArgs 
                 const bool all = (valid.x & valid.y) == 0xffffffffu, whole = i >= lo && i < hi && all;
                 if (!all) {
                     // rows that are no entry of the axis (behind the end of a page's use) hold anything, and 0 x NaN is NaN
-                    const int at = kvn + value_place(mode, nt, i, s), slot = at % NS;
+                    const int at = kvn + value_place(mode, rounds_of(mode, nt), mode == STEPS ? i >> 1 : i, s), slot = at % NS;
                     if (!(go = warp_wait(smem_at(&sh.full[slot]), (at / NS) & 1, quit))) break;
                     if (!(((row & 32 ? valid.y : valid.x) >> lane) & 1)) {           // two threads to a row of values
                         char* slot_at = kv_s + slot * S::SLOT;
@@ -1145,6 +1160,9 @@ cudaError_t launch(const HxCore& core, AttendArgs a, cudaStream_t s) {
     a.row_tiles = hx_ceil_div(a.max_q * a.group, GROUP_ROWS);
     const int64_t items = (int64_t)a.n * a.row_tiles;
     a.planned = items <= PLAN_ITEMS;
+    // Two heads to a block spare the joining of two streams (256 decoding sequences of 8 heads: 617 us against 720), alternate steps
+    // of one spread few groups further (4 sequences: 24 us against 33).
+    a.twin = items * (a.n_kv_heads / 2) >= core.n_sm;
     cudaError_t e = hx_opt_in_smem(hx_attend_kernel<D, T>, Shape<D>::SMEM, allowed, 0);
     if (e != cudaSuccess) return e;
     const int blocks = std::min(core.n_sm, MAX_BLOCKS);

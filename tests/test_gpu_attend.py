@@ -285,6 +285,25 @@ def test_tree_refusals(hx, cluster):
     assert cluster.status() == 0
 
 
+@pytest.mark.parametrize("dim, heads, t", [(128, 8, 21), (128, 3, 40), (64, 8, 21), (128, 1, 9)])
+def test_ragged_trees_share_blocks(hx, cluster, dim, heads, t):
+    """More groups than multiprocessors, of all lengths, so that blocks go from one to the next in the middle of others."""
+    rng = random.Random(heads)
+    n = 24 if heads == 8 else 48
+    lengths = [rng.choice((0, 1, 30, 64, 65, 130, 200, 333, 600, 900)) for _ in range(n)]
+    check_tree(hx, cluster, lengths, [random_tree(rng, t, absent=(i % 4 == 3) * (t // 4)) for i in range(n)], q_heads=heads * 4, heads=heads, dim=dim, page=24,
+               dtype=torch.float16, seed=heads)
+
+
+@pytest.mark.parametrize("dim, heads, group", [(128, 2, 4), (64, 1, 7), (128, 5, 2)])
+def test_prompts_beside_decoding(hx, cluster, dim, heads, group):
+    """Groups of one row, of up to 128 and of more, one after another in the same blocks."""
+    rng = random.Random(group)
+    lengths = [rng.choice((1, 5, 64, 100, 150, 260, 400)) for _ in range(36)]
+    counts = [min(n, rng.choice((1, 1, 1, 9, 31, 70, 150))) for n in lengths]
+    check_window(hx, cluster, lengths, counts, 120, 3, q_heads=heads * group, heads=heads, dim=dim, page=16, seed=group)
+
+
 # --- how a program uses them -----------------------------------------------------------------------------------
 
 
