@@ -47,6 +47,7 @@ constexpr int PLAN_ITEMS = 1024;     // groups per head that the shared plan hol
 // Units of the line that is cut into shares: what a step costs both streams, what it costs when they take alternate ones, and what
 // the start and end of a group cost (measured: some 2,300, 1,500 and 7,000 cycles).
 constexpr int BOTH_COST = 3, ALTERNATE_COST = 2, GROUP_COST = 8;
+constexpr int SHORT_LINE = 24;       // units to a block below which groups are cut without regard to their cost: what counts is the longest chain
 constexpr int SEGS = 2;              // groups looked up ahead
 constexpr int VALID_RING = 16;
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
@@ -231,39 +232,50 @@ __device__ __forceinline__ int head_steps(const AttendArgs& a, int rows) { retur
 
 // The line of steps: prefix[i] = units before item i.
 __device__ __forceinline__ int step_cost(const AttendArgs& a, int rows) { return rows > TILE_ROWS || (a.twin && a.n_kv_heads > 1) ? BOTH_COST : ALTERNATE_COST; }
-struct Plan { int64_t total; int shares; };
-__device__ Plan make_plan(const AttendArgs& a, int64_t* prefix, int64_t* scan, int n_blocks, bool report) {
+struct Plan { int64_t total; int shares, group_cost; };
+__device__ Plan make_plan(const AttendArgs& a, int64_t* prefix, int* count, int64_t* scan, int n_blocks, bool report) {
     const int tid = threadIdx.x, nt = blockDim.x, lane = tid & 31, warp = tid >> 5, items = a.n * a.row_tiles;
     const int per = hx_ceil_div(items, nt), i0 = min(items, tid * per), i1 = min(items, i0 + per);
-    int64_t sum = 0;
+    int64_t sum = 0, groups = 0;
     for (int i = i0; i < i1; ++i) {
         const Group g = group_of(a, i, 0, report);
-        const int64_t u = g.steps ? ((int64_t)g.steps * step_cost(a, g.rows) + GROUP_COST) * head_steps(a, g.rows) : 0;
-        prefix[i] = u; sum += u;
+        const int heads = g.steps ? head_steps(a, g.rows) : 0;
+        prefix[i] = (int64_t)g.steps * step_cost(a, g.rows) * heads; sum += prefix[i];
+        count[i] = heads; groups += heads;
     }
-    int64_t incl = sum;
+    int64_t incl = sum, incl_g = groups;
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) { const int64_t t = __shfl_up_sync(0xffffffffu, incl, o); if (lane >= o) incl += t; }
-    if (lane == 31) scan[warp] = incl;
+    for (int o = 1; o < 32; o <<= 1) {
+        const int64_t t = __shfl_up_sync(0xffffffffu, incl, o), q = __shfl_up_sync(0xffffffffu, incl_g, o);
+        if (lane >= o) { incl += t; incl_g += q; }
+    }
+    if (lane == 31) { scan[2 * warp] = incl; scan[2 * warp + 1] = incl_g; }
     __syncthreads();
-    int64_t before = incl - sum, all = 0;
-    for (int w = 0; w < nt / 32; ++w) { if (w < warp) before += scan[w]; all += scan[w]; }
-    for (int i = i0; i < i1; ++i) { const int64_t u = prefix[i]; prefix[i] = before; before += u; }
-    if (tid == 0) prefix[items] = all;
-    __syncthreads();
+    int64_t before = incl - sum, before_g = incl_g - groups, all = 0, all_g = 0;
+    for (int w = 0; w < nt / 32; ++w) {
+        if (w < warp) { before += scan[2 * w]; before_g += scan[2 * w + 1]; }
+        all += scan[2 * w]; all_g += scan[2 * w + 1];
+    }
     Plan p;
-    p.total = all;
+    p.group_cost = all < (int64_t)n_blocks * SHORT_LINE ? 0 : GROUP_COST;
+    before += before_g * p.group_cost;
+    for (int i = i0; i < i1; ++i) { const int64_t u = prefix[i] + (int64_t)count[i] * p.group_cost; prefix[i] = before; before += u; }
+    p.total = all + all_g * p.group_cost;
+    if (tid == 0) prefix[items] = p.total;
+    __syncthreads();
     // a share holds at least one step of every group that begins before it and ends behind it
-    p.shares = (int)min((int64_t)n_blocks, max((int64_t)1, p.total / (GROUP_COST + BOTH_COST)));
+    p.shares = (int)min((int64_t)n_blocks, max((int64_t)1, p.total / (p.group_cost + BOTH_COST)));
     return p;
 }
 
 // A walk over the groups of block `block`.
 struct Walk {
     int64_t unit, end, step;
+    int group_cost;
 };
 __device__ __forceinline__ Walk begin_walk(const AttendArgs& a, const Plan& p, int block, int n_blocks) {
     Walk w;
+    w.group_cost = p.group_cost;
     if (a.planned) {
         w.unit = block < p.shares ? hx_share(p.total, block, p.shares) : 0;
         w.end = block < p.shares ? hx_share(p.total, block + 1, p.shares) : 0;
@@ -295,10 +307,10 @@ __device__ __forceinline__ bool next_group(const AttendArgs& a, const int64_t* p
         const int64_t x = in - at * units, left = min(units - x, w.end - u);
         w.unit = u + left;
         if (at) *g = group_of(a, lo, g->rows > TILE_ROWS || !a.twin ? at : 2 * at);
-        const int cost = step_cost(a, g->rows);             // step i belongs to the share of unit GROUP_COST + i * cost
-        *t0 = (int)((max((int64_t)0, x - GROUP_COST) + cost - 1) / cost);
-        *t1 = min((int)((max((int64_t)0, x + left - GROUP_COST) + cost - 1) / cost), g->steps);
-        *start = u - x + GROUP_COST;
+        const int cost = step_cost(a, g->rows);             // step i belongs to the share of unit group_cost + i * cost
+        *t0 = (int)((max((int64_t)0, x - w.group_cost) + cost - 1) / cost);
+        *t1 = min((int)((max((int64_t)0, x + left - w.group_cost) + cost - 1) / cost), g->steps);
+        *start = u - x + w.group_cost;
         if (*t1 > *t0) return true;
     }
     return false;
@@ -426,7 +438,7 @@ __device__ __forceinline__ uint32_t piece(int r, int c, int rows) { return (uint
 struct Shared {
     Seg seg[SEGS];
     int64_t prefix[PLAN_ITEMS + 1];
-    int64_t scan[THREADS / 32];
+    int64_t scan[THREADS / 16];
     alignas(16) uint32_t valid[2][VALID_RING][2];        // entries of a step that have a row, of each of two heads
     float2 stat[2][TILE_ROWS];          // maximum and sum of the second stream, where it shares its rows
     alignas(16) float buf[8 * 512];  // results on their way out, 2 KB to a warp; a stream's four also join the copies of rows
@@ -577,7 +589,7 @@ __global__ void __launch_bounds__(THREADS, 1) hx_attend_kernel(const AttendArgs 
     hx_wait_for_primary();
     if (tid == 0) a.desc[blockIdx.x] = make_int4(0, 0, 0, 0);
     Plan plan{};
-    if (a.planned) plan = make_plan(a, sh.prefix, sh.scan, gridDim.x, blockIdx.x == 0);
+    if (a.planned) plan = make_plan(a, sh.prefix, reinterpret_cast<int*>(sh.buf), sh.scan, gridDim.x, blockIdx.x == 0);
     tc_before();
     __syncthreads();
     tc_after();
@@ -1075,14 +1087,15 @@ constexpr int JOIN_THREADS = 256;
 template <int D, class T>
 __global__ void __launch_bounds__(JOIN_THREADS) hx_attend_join_kernel(const AttendArgs a) {
     hx_wait_for_primary();
-    __shared__ int64_t prefix[PLAN_ITEMS + 1], scan[JOIN_THREADS / 32];
+    __shared__ int64_t prefix[PLAN_ITEMS + 1], scan[JOIN_THREADS / 16];
+    __shared__ int count[PLAN_ITEMS];
     __shared__ uint4 anc[HX_TREE_MAX];
     __shared__ int link[HX_TREE_MAX];
     const int4 de = a.desc[blockIdx.x];
     const int tid = threadIdx.x;
     if (de.w) {
         Plan plan{};
-        if (a.planned) plan = make_plan(a, prefix, scan, gridDim.x, false);
+        if (a.planned) plan = make_plan(a, prefix, count, scan, gridDim.x, false);
         Walk w = begin_walk(a, plan, blockIdx.x, gridDim.x);
         Group g;
         int t0, t1;
@@ -1147,9 +1160,22 @@ bool encode(CUtensorMap* map, const char* base, int64_t width, int64_t rows, int
                      CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// A kernel between two launches of the one that takes all shared memory asks for the same split of it, once per device: the
+// multiprocessor would change it, and back, otherwise.
+template <class Kernel>
+cudaError_t same_carveout(Kernel kernel, bool* asked) {
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess || asked[dev & 63]) return e;
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
+    if (e == cudaSuccess) asked[dev & 63] = true;
+    return e;
+}
+
 template <int D, class T>
 cudaError_t launch(const HxCore& core, AttendArgs a, cudaStream_t s) {
     static size_t allowed[64];
+    static bool joined[64];
     Maps maps{};
     if (!encoder()) return cudaErrorNotSupported;
     const int64_t width = (int64_t)a.n_kv_heads * D, rows = (int64_t)(a.n_pages - 1) * a.page_rows + a.page_tokens;
@@ -1169,6 +1195,8 @@ cudaError_t launch(const HxCore& core, AttendArgs a, cudaStream_t s) {
     e = hx_launch_dependent(hx_attend_kernel<D, T>, dim3(blocks), dim3(THREADS), Shape<D>::SMEM, s, a, maps);
     if (e != cudaSuccess) return e;
     ++*core.launches;
+    e = same_carveout(hx_attend_join_kernel<D, T>, joined);
+    if (e != cudaSuccess) return e;
     e = hx_launch_dependent(hx_attend_join_kernel<D, T>, dim3(blocks), dim3(JOIN_THREADS), 0, s, a);
     if (e == cudaSuccess) ++*core.launches;
     return e;

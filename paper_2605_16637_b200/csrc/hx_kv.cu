@@ -198,7 +198,7 @@ __device__ __forceinline__ void move16(uint4* dst, const uint4* src, int64_t n) 
     }
 }
 
-// One row of the table, by the block.  In place every element is read and written by the same thread, and a row that is
+// One row of the table, by a warp.  In place every element is read and written by the same thread, and a row that is
 // read by a fork is rewritten by no other request.
 __device__ void apply_row(const PlanArgs& p, int s, bool elsewhere) {
     const int i = p.w.owner[s];
@@ -226,7 +226,8 @@ __device__ void apply_row(const PlanArgs& p, int s, bool elsewhere) {
             from = p.in.table + (int64_t)r * p.max_pages;
         }
     }
-    for (int c = threadIdx.x; c < p.max_pages; c += blockDim.x) {
+    const int lane = threadIdx.x & 31;
+    for (int c = lane; c < p.max_pages; c += 32) {
         const int old = p.in.table[at + c];
         int now = old;
         if (c < full) now = i >= 0 ? from[c] : old;
@@ -238,22 +239,20 @@ __device__ void apply_row(const PlanArgs& p, int s, bool elsewhere) {
         }
         if (elsewhere || now != old) p.out.table[at + c] = now;
     }
-    __syncthreads();                                           // everybody has read the length
-    if (threadIdx.x == 0) p.out.len[s] = new_len;
+    __syncwarp();                                              // everybody has read the length
+    if (lane == 0) p.out.len[s] = new_len;
 }
 
-// Items [0, max_seqs) are rows of the table; behind them a fork has one item per request and plane (keys or values of a
-// layer), a copy one per page that the target takes and plane.
+// A warp to each row of the table first (a chain of four dependent loads: as many rows as fit are in flight), then a block to each
+// piece of data: of a fork one per request and plane (keys or values of a layer), of a copy one per page that the target takes and plane.
 __global__ void __launch_bounds__(256) hx_kv_apply_kernel(PlanArgs p, DataArgs d, int elsewhere) {
     hx_wait_for_primary();
     const int planes = 2 * d.n_layers;
     int64_t data = 0;
     if (p.op == KV_FORK) data = (int64_t)p.n * planes;
     if (p.op == KV_COPY) data = (int64_t)p.w.count[0] * planes;
-    const int64_t items = p.max_seqs + data;
-    for (int64_t it = blockIdx.x; it < items; it += gridDim.x) {
-        if (it < p.max_seqs) { apply_row(p, (int)it, elsewhere != 0); continue; }
-        const int64_t e = it - p.max_seqs;
+    for (int s = blockIdx.x * 8 + (threadIdx.x >> 5); s < p.max_seqs; s += gridDim.x * 8) apply_row(p, s, elsewhere != 0);
+    for (int64_t e = gridDim.x - 1 - blockIdx.x; e < data; e += gridDim.x) {
         const int plane = (int)(e % planes), layer = plane >> 1, g = (int)(e / planes);
         uint4* to = (plane & 1 ? d.v : d.k) + layer * d.layer16;
         if (p.op == KV_FORK) {
@@ -319,32 +318,32 @@ __global__ void __launch_bounds__(PLAN_THREADS) hx_kv_pack_plan_kernel(const int
     if (tid == 0) { w.count[0] = used - below; w.count[1] = used; }
 }
 
-// Items: first the rows of the table (one each), then chunks of the counts, then one item per page that moves and plane.
+// A warp to each row of the table, then items: chunks of the counts, and one per page that moves and plane.
 constexpr int PACK_CHUNK = 1024;
 __global__ void __launch_bounds__(256) hx_kv_pack_apply_kernel(KvTab in, KvTab out, int n_pages, int max_seqs, int max_pages, int page_tokens,
                                                                KvWork w, const int32_t* goes, DataArgs d, int elsewhere) {
     hx_wait_for_primary();
     const int planes = 2 * d.n_layers, moved = w.count[0], used = w.count[1];
-    const int64_t chunks = hx_ceil_div(n_pages, PACK_CHUNK), small = max_seqs + chunks;
-    const int64_t items = small + (int64_t)moved * planes;
+    const int64_t chunks = hx_ceil_div(n_pages, PACK_CHUNK), items = chunks + (int64_t)moved * planes;
     const int32_t *src = w.pages, *dst = w.pages + n_pages / 2;
+    for (int s = blockIdx.x * 8 + (threadIdx.x >> 5); s < max_seqs; s += gridDim.x * 8) {
+        for (int c = threadIdx.x & 31; c < max_pages; c += 32) {
+            const int64_t at = (int64_t)s * max_pages + c;
+            const int old = in.table[at], now = (old >= 0 && old < n_pages) ? goes[old] : old;
+            if (elsewhere || now != old) out.table[at] = now;
+        }
+        if (elsewhere && (threadIdx.x & 31) == 0) out.len[s] = in.len[s];
+    }
     for (int64_t it = blockIdx.x; it < items; it += gridDim.x) {
-        if (it < max_seqs) {
-            for (int c = threadIdx.x; c < max_pages; c += blockDim.x) {
-                const int64_t at = it * max_pages + c;
-                const int old = in.table[at], now = (old >= 0 && old < n_pages) ? goes[old] : old;
-                if (elsewhere || now != old) out.table[at] = now;
-            }
-            if (elsewhere && threadIdx.x == 0) out.len[it] = in.len[it];
-        } else if (it < small) {
-            const int p0 = (int)(it - max_seqs) * PACK_CHUNK;
+        if (it < chunks) {
+            const int p0 = (int)it * PACK_CHUNK;
             for (int q = p0 + threadIdx.x; q < min(n_pages, p0 + PACK_CHUNK); q += blockDim.x) {
                 const int g = goes[q];
                 if (g == q || (g < 0 && q >= used)) { if (elsewhere) out.ref[q] = in.ref[q]; }
                 else if (g >= 0) { out.ref[g] = in.ref[q]; out.ref[q] = 0; }      // the free number's own thread writes nothing
             }
         } else {
-            const int64_t e = it - small;
+            const int64_t e = it - chunks;
             const int plane = (int)(e % planes), m = (int)(e / planes);
             uint4* to = (plane & 1 ? d.v : d.k) + (plane >> 1) * d.layer16;
             move16<4>(to + dst[m] * d.page16, to + src[m] * d.page16, page_tokens * d.token16);
@@ -431,9 +430,9 @@ cudaError_t launch_op(const HxCore& core, const PlanArgs& p, const DataArgs& d, 
     e = hx_launch_dependent(hx_kv_plan_kernel, dim3(1 + copiers), dim3(PLAN_THREADS), plan_smem(p.max_seqs), s, p);
     if (e != cudaSuccess) return e;
     ++*core.launches;
-    int64_t items = p.max_seqs;
-    if (p.op == KV_FORK) items += (int64_t)p.n * 2 * d.n_layers;
-    if (p.op == KV_COPY) items += (int64_t)p.n_pages * 2 * d.n_layers;       // at most: the number is on the device
+    int64_t items = hx_ceil_div(p.max_seqs, 8);
+    if (p.op == KV_FORK) items = std::max<int64_t>(items, (int64_t)p.n * 2 * d.n_layers);
+    if (p.op == KV_COPY) items = std::max<int64_t>(items, (int64_t)p.n_pages * 2 * d.n_layers);      // at most: the number is on the device
     const int grid = (int)std::min<int64_t>(items, (int64_t)core.n_sm * 8);
     e = hx_launch_dependent(hx_kv_apply_kernel, dim3(grid), dim3(256), 0, s, p, d, (int)elsewhere);
     if (e == cudaSuccess) ++*core.launches;
@@ -574,7 +573,7 @@ int hx_kv_compact(hx_cluster* h, const hx_kv_cache* cache, const hx_kv_tables* o
     if (e != cudaSuccess) return done(h, e, "packing kernels");
     ++*core.launches;
     const DataArgs d = data_of(cache);
-    const int64_t items = cache->max_seqs + hx_ceil_div(cache->n_pages, PACK_CHUNK) + (int64_t)(cache->n_pages / 2) * 2 * d.n_layers;
+    const int64_t items = std::max<int64_t>(hx_ceil_div(cache->max_seqs, 8), hx_ceil_div(cache->n_pages, PACK_CHUNK) + (int64_t)(cache->n_pages / 2) * 2 * d.n_layers);
     e = hx_launch_dependent(hx_kv_pack_apply_kernel, dim3((unsigned)std::min<int64_t>(items, (int64_t)core.n_sm * 8)), dim3(256), 0, s, tab_of(cache),
                             tab_of(out, cache), cache->n_pages, cache->max_seqs, cache->max_pages, cache->page_tokens, w, out_goes, d, (int)elsewhere);
     if (e == cudaSuccess) ++*core.launches;
