@@ -36,8 +36,8 @@ extern "C" {
 #define HX_ERR_CUDA         (-2)   /* a CUDA runtime call failed; message holds cudaGetErrorString */
 #define HX_ERR_CYCLE        (-3)   /* the uploaded graph is not acyclic */
 #define HX_ERR_NOT_READY    (-4)   /* scoring needs horizons but hx_critical_path was not enqueued */
-#define HX_ERR_TIMEOUT      (-5)   /* reserved for a bounded device-side wait that runs out; no entry point of
-                                      this version waits on the device, so the code is never returned */
+#define HX_ERR_TIMEOUT      (-5)   /* a bounded device-side wait ran out (some two seconds): raised in the status word
+                                      by the attention kernels, whose output is then incomplete; no call returns it */
 #define HX_ERR_OOM          (-6)   /* host or device allocation failed */
 
 /* out_cost of hx_schedule_batch (Delta = earliest projected decode finish of the call) */
@@ -643,8 +643,10 @@ int hx_kv_compact(hx_cluster* h, const hx_kv_cache* cache, const hx_kv_tables* o
  * copy to the host.  Needs a pool of less than 2^24 tokens. */
 int hx_kv_report(hx_cluster* h, const hx_kv_cache* cache, int decode_instance, void* stream);
 
-/* Attention over a paged cache (F16 or BF16; head_dim 64, 96 or 128; n_q_heads a multiple of
- * n_kv_heads, query head h reads KV head h / (n_q_heads / n_kv_heads)):
+/* Attention over a paged cache (F16 or BF16; head_dim 64, 96 or 128; n_q_heads 1 to 128 times
+ * n_kv_heads, query head h reads KV head h / (n_q_heads / n_kv_heads); page_stride a whole number of tokens, less
+ * than 2^31 tokens from the first page to the last).  Pages of any size will do; those whose size has a power of two of 16
+ * or more as a factor are read fastest:
  *   out = sum_j softmax_j(scale * q . k_j) v_j,  lse = log sum_j exp(scale * q . k_j)
  * over the rows j that a query sees.  Sums, maxima and the result are held in binary32; the weights
  * are rounded to the element type for the product with the values.  A query that sees
