@@ -384,14 +384,14 @@ __device__ __forceinline__ uint32_t below(int n) { return n <= 0 ? 0u : n >= 32 
 
 // What a row sees of its group's axis.  Window: entries below `first`, and [lo, hi).  Tree: entries below lo (`first` = 0: the token is
 // not there and sees nothing), and its ancestors among the drafted ones from lo on.
-struct View { int first, lo, hi; uint4 anc; };
+struct View { int first, lo, hi; const uint4* anc; };
 __device__ __forceinline__ View view_of(const AttendArgs& a, const Group& g, const uint4* anc, int r) {
     const int qi = (g.r0 + r) / a.group;
     View v;
-    v.anc = make_uint4(0, 0, 0, 0);
+    v.anc = anc + (a.tree ? qi : 0);
     if (a.tree) {
-        v.anc = anc[qi];
-        v.first = (v.anc.x | v.anc.y | v.anc.z | v.anc.w) != 0;
+        const uint4 m = *v.anc;
+        v.first = (m.x | m.y | m.z | m.w) != 0;
         v.lo = g.axis.n_sink; v.hi = 0;
         return v;
     }
@@ -405,7 +405,8 @@ __device__ __forceinline__ View view_of(const AttendArgs& a, const Group& g, con
 template <int W>
 __device__ __forceinline__ void sees(int tree, const View& v, int xa, uint32_t (&m)[W]) {
     if (tree) {
-        const uint32_t w[5] = {v.anc.x, v.anc.y, v.anc.z, v.anc.w, 0u};
+        const uint4 t = *v.anc;
+        const uint32_t w[5] = {t.x, t.y, t.z, t.w, 0u};
 #pragma unroll
         for (int i = 0; i < W; ++i) {
             const int s = xa + 32 * i - v.lo;            // drafted token of the word's first bit
