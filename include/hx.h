@@ -653,7 +653,8 @@ int hx_kv_report(hx_cluster* h, const hx_kv_cache* cache, int decode_instance, v
  * nothing gets zeros and lse -inf; rows that a query does not see have no part in its result whatever they hold
  * (infinities and NaN too).
  *   q, out: element (row, head, i) at row * row_stride + head * head_stride + i; q 16-byte
- * aligned with strides that are multiples of 8 elements, out 4-byte aligned with even strides.  lse:
+ * aligned with strides that are multiples of 8 elements, out 4-byte aligned with even strides.  out and lse overlap nothing
+ * that the call reads.  lse:
  * binary32 [n_rows][n_q_heads] or NULL.  work: hx_attend_work bytes, 16-byte aligned, free to use again when the
  * call's work is done; calls that may overlap on the GPU need one each.
  *   seqs: device int32[n], the cache's sequences.  A sequence with an id or length out of range raises

@@ -1233,6 +1233,7 @@ const char* why_not_io(const hx_kv_cache* c, int layer, const hx_attend_io* io, 
     if (n < 0 || io->n_rows < 0) return "negative number of sequences or rows";
     if (n > (1 << 20)) return "more than 2^20 sequences in one call";
     if (!io->q || !io->out || !io->work) return "NULL buffer";
+    if (io->q == io->out) return "out must not be q";             // rows of q may be read again for results that are not finite
     if (!(io->scale > 0.f) || !(io->scale < 1e30f)) return "scale must be finite and above zero";
     if (reinterpret_cast<uintptr_t>(io->q) % 16 || io->q_row_stride % 8 || io->q_head_stride % 8) return "q must be 16-byte aligned with strides that are multiples of 8";
     if (reinterpret_cast<uintptr_t>(io->out) % 4 || io->out_row_stride % 2 || io->out_head_stride % 2) return "out must be 4-byte aligned with even strides";
@@ -1295,6 +1296,8 @@ int hx_attend_window(hx_cluster* h, const hx_kv_cache* cache, int layer, const h
     if (!why && n && (!seqs || !cu)) why = "NULL buffer";
     if (!why && (max_q < 0 || max_q > (1 << 23))) why = "max_q must be 0 to 2^23";
     if (!why && (window < 0 || sinks < 0)) why = "window and sinks must not be negative";
+    if (!why && n && (int64_t)n * hx_ceil_div(max_q * (io->n_q_heads / cache->n_kv_heads), GROUP_ROWS) >= (1LL << 31))
+        why = "n times max_q is too large: 2^31 groups of 256 rows or more";       // groups are numbered in 32 bits
     if (why) return hx_fail(h, HX_ERR_INVALID_ARG, why);
     if (n == 0 || max_q == 0 || io->n_rows == 0) return HX_OK;
     const HxCore core = hx_core(h);

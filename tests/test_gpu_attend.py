@@ -377,3 +377,16 @@ def test_draft_verify_accept_step(hx, cluster):
     cluster.kv_free(cache, ints(seqs))
     pool.drop(seqs)
     assert cache.ref.tolist() == pool.ref == [0] * 40 and cluster.status() == 0
+
+
+def test_in_place_and_too_many_groups_are_refused(hx, cluster):
+    """Both on the host, before anything runs: a result over q, and groups whose numbers pass 32 bits (2^16 sequences of up to 2^23 queries)."""
+    cache = hx.KvCache(**make_pool(3, [40], **spread([40], 16)))
+    q = torch.randn(4, 4, 64, device="cuda").bfloat16()
+    before = q.clone()
+    with pytest.raises(hx.HxError, match="out must not be q"):
+        cluster.attend_window(cache, 0, q, ints([0]), ints([0, 4]), 4, 8, out=q)
+    n = 1 << 16
+    with pytest.raises(hx.HxError, match="too large"):
+        cluster.attend_window(cache, 0, q, torch.zeros(n, dtype=torch.int32, device="cuda"), torch.zeros(n + 1, dtype=torch.int32, device="cuda"), 1 << 23, 8)
+    assert torch.equal(q, before) and cluster.status() == 0
