@@ -45,9 +45,10 @@ constexpr int THREADS = 512;
 constexpr int LOADERS = 4;           // warps that load keys and values
 constexpr int PLAN_ITEMS = 1024;     // groups per head that the shared plan holds
 // Units of the line that is cut into shares: what a step costs both streams, what it costs when they take alternate ones, and what
-// the start and end of a group cost (measured: some 2,300, 1,500 and 7,000 cycles).
+// the start and end of a group cost.  A step of 256 rows and head_dim 128 takes some 2,300 cycles (1.17 us: two groups to a
+// multiprocessor, 32 steps more in each: 75 us).  Cutting short lines as if groups cost nothing was slower: one tree of 8 tokens 49
+// us against 42, 4 decoding sequences 32 against 30.
 constexpr int BOTH_COST = 3, ALTERNATE_COST = 2, GROUP_COST = 8;
-constexpr int SHORT_LINE = 24;       // units to a block below which groups are cut without regard to their cost: what counts is the longest chain
 constexpr int SEGS = 2;              // groups looked up ahead
 constexpr int VALID_RING = 16;
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
@@ -232,50 +233,39 @@ __device__ __forceinline__ int head_steps(const AttendArgs& a, int rows) { retur
 
 // The line of steps: prefix[i] = units before item i.
 __device__ __forceinline__ int step_cost(const AttendArgs& a, int rows) { return rows > TILE_ROWS || (a.twin && a.n_kv_heads > 1) ? BOTH_COST : ALTERNATE_COST; }
-struct Plan { int64_t total; int shares, group_cost; };
-__device__ Plan make_plan(const AttendArgs& a, int64_t* prefix, int* count, int64_t* scan, int n_blocks, bool report) {
+struct Plan { int64_t total; int shares; };
+__device__ Plan make_plan(const AttendArgs& a, int64_t* prefix, int64_t* scan, int n_blocks, bool report) {
     const int tid = threadIdx.x, nt = blockDim.x, lane = tid & 31, warp = tid >> 5, items = a.n * a.row_tiles;
     const int per = hx_ceil_div(items, nt), i0 = min(items, tid * per), i1 = min(items, i0 + per);
-    int64_t sum = 0, groups = 0;
+    int64_t sum = 0;
     for (int i = i0; i < i1; ++i) {
         const Group g = group_of(a, i, 0, report);
-        const int heads = g.steps ? head_steps(a, g.rows) : 0;
-        prefix[i] = (int64_t)g.steps * step_cost(a, g.rows) * heads; sum += prefix[i];
-        count[i] = heads; groups += heads;
+        const int64_t u = g.steps ? ((int64_t)g.steps * step_cost(a, g.rows) + GROUP_COST) * head_steps(a, g.rows) : 0;
+        prefix[i] = u; sum += u;
     }
-    int64_t incl = sum, incl_g = groups;
+    int64_t incl = sum;
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const int64_t t = __shfl_up_sync(0xffffffffu, incl, o), q = __shfl_up_sync(0xffffffffu, incl_g, o);
-        if (lane >= o) { incl += t; incl_g += q; }
-    }
-    if (lane == 31) { scan[2 * warp] = incl; scan[2 * warp + 1] = incl_g; }
+    for (int o = 1; o < 32; o <<= 1) { const int64_t t = __shfl_up_sync(0xffffffffu, incl, o); if (lane >= o) incl += t; }
+    if (lane == 31) scan[warp] = incl;
     __syncthreads();
-    int64_t before = incl - sum, before_g = incl_g - groups, all = 0, all_g = 0;
-    for (int w = 0; w < nt / 32; ++w) {
-        if (w < warp) { before += scan[2 * w]; before_g += scan[2 * w + 1]; }
-        all += scan[2 * w]; all_g += scan[2 * w + 1];
-    }
+    int64_t before = incl - sum, all = 0;
+    for (int w = 0; w < nt / 32; ++w) { if (w < warp) before += scan[w]; all += scan[w]; }
+    for (int i = i0; i < i1; ++i) { const int64_t u = prefix[i]; prefix[i] = before; before += u; }
+    if (tid == 0) prefix[items] = all;
+    __syncthreads();
     Plan p;
-    p.group_cost = all < (int64_t)n_blocks * SHORT_LINE ? 0 : GROUP_COST;
-    before += before_g * p.group_cost;
-    for (int i = i0; i < i1; ++i) { const int64_t u = prefix[i] + (int64_t)count[i] * p.group_cost; prefix[i] = before; before += u; }
-    p.total = all + all_g * p.group_cost;
-    if (tid == 0) prefix[items] = p.total;
-    __syncthreads();
+    p.total = all;
     // a share holds at least one step of every group that begins before it and ends behind it
-    p.shares = (int)min((int64_t)n_blocks, max((int64_t)1, p.total / (p.group_cost + BOTH_COST)));
+    p.shares = (int)min((int64_t)n_blocks, max((int64_t)1, p.total / (GROUP_COST + BOTH_COST)));
     return p;
 }
 
 // A walk over the groups of block `block`.
 struct Walk {
     int64_t unit, end, step;
-    int group_cost;
 };
 __device__ __forceinline__ Walk begin_walk(const AttendArgs& a, const Plan& p, int block, int n_blocks) {
     Walk w;
-    w.group_cost = p.group_cost;
     if (a.planned) {
         w.unit = block < p.shares ? hx_share(p.total, block, p.shares) : 0;
         w.end = block < p.shares ? hx_share(p.total, block + 1, p.shares) : 0;
@@ -307,10 +297,10 @@ __device__ __forceinline__ bool next_group(const AttendArgs& a, const int64_t* p
         const int64_t x = in - at * units, left = min(units - x, w.end - u);
         w.unit = u + left;
         if (at) *g = group_of(a, lo, g->rows > TILE_ROWS || !a.twin ? at : 2 * at);
-        const int cost = step_cost(a, g->rows);             // step i belongs to the share of unit group_cost + i * cost
-        *t0 = (int)((max((int64_t)0, x - w.group_cost) + cost - 1) / cost);
-        *t1 = min((int)((max((int64_t)0, x + left - w.group_cost) + cost - 1) / cost), g->steps);
-        *start = u - x + w.group_cost;
+        const int cost = step_cost(a, g->rows);             // step i belongs to the share of unit GROUP_COST + i * cost
+        *t0 = (int)((max((int64_t)0, x - GROUP_COST) + cost - 1) / cost);
+        *t1 = min((int)((max((int64_t)0, x + left - GROUP_COST) + cost - 1) / cost), g->steps);
+        *start = u - x + GROUP_COST;
         if (*t1 > *t0) return true;
     }
     return false;
@@ -439,7 +429,7 @@ __device__ __forceinline__ uint32_t piece(int r, int c, int rows) { return (uint
 struct Shared {
     Seg seg[SEGS];
     int64_t prefix[PLAN_ITEMS + 1];
-    int64_t scan[THREADS / 16];
+    int64_t scan[THREADS / 32];
     alignas(16) uint32_t valid[2][VALID_RING][2];        // entries of a step that have a row, of each of two heads
     float2 stat[2][TILE_ROWS];          // maximum and sum of the second stream, where it shares its rows
     alignas(16) float buf[8 * 512];  // results on their way out, 2 KB to a warp; a stream's four also join the copies of rows
@@ -590,7 +580,7 @@ __global__ void __launch_bounds__(THREADS, 1) hx_attend_kernel(const AttendArgs 
     hx_wait_for_primary();
     if (tid == 0) a.desc[blockIdx.x] = make_int4(0, 0, 0, 0);
     Plan plan{};
-    if (a.planned) plan = make_plan(a, sh.prefix, reinterpret_cast<int*>(sh.buf), sh.scan, gridDim.x, blockIdx.x == 0);
+    if (a.planned) plan = make_plan(a, sh.prefix, sh.scan, gridDim.x, blockIdx.x == 0);
     tc_before();
     __syncthreads();
     tc_after();
@@ -677,77 +667,77 @@ __global__ void __launch_bounds__(THREADS, 1) hx_attend_kernel(const AttendArgs 
         if (warp < 10) {
             // ---- products of one stream: one thread, as every instruction of this loop is on the way from weights to scores
             if (lane == 0) {
-            constexpr uint32_t QK = product(Elem<T>::FORMAT, STEP, false), PV = product(Elem<T>::FORMAT, D, true);
-            const int s = warp - 8;
-            const uint32_t q_m = matrix(smem_at(q_s), 16), k_m = matrix(smem_at(kv_s), 16), v_m = matrix(smem_at(kv_s), 8192);
-            const uint32_t S_at = tmem + s * 128, O_at = tmem + 256 + s * 128;
-            const uint32_t full = smem_at(&sh.full[0]), empty = smem_at(&sh.empty[0]), s_full = smem_at(&sh.s_full[s][0]), p_full = smem_at(&sh.p_full[s][0]);
-            int kvn = 0, sn = 0;                         // loads before the group, steps of this stream so far
-            bool go = true;
-            for (int n = 0; go; ++n) {
-                const int si = n % SEGS;
-                if (!(go = bar_wait(smem_at(&sh.seg_full[si]), (n / SEGS) & 1, quit))) break;
-                const int nt = sh.seg[si].t1 - sh.seg[si].t0;
-                const Mode mode = mode_of(sh.seg[si].g);
-                bar_arrive(smem_at(&sh.seg_empty[si]));
-                if (nt <= 0) break;
-                if (!(go = bar_wait(smem_at(&sh.q_full), n & 1, quit))) break;
-                const uint32_t q_t = q_m + (mode == STEPS ? 0 : s) * (S::TILE >> 4);
-                const int rounds = rounds_of(mode, nt), own = mode == STEPS ? (nt + 1 - s) / 2 : nt;         // this stream's steps
-                const bool alone = mode != ROWS;         // a slot that this stream reads alone is given back for the other one too
-                // scores of this stream's step i: number k of all, into buffer k & 1
-                auto scores = [&](int i, int k) {
-                    const int at = kvn + key_place(mode, i, s), slot = at % NS;
-                    if (!bar_wait(full + slot * 8, (at / NS) & 1, quit)) return false;
-                    tc_after();
-                    const uint32_t k_t = k_m + slot * (S::SLOT >> 4), to = S_at + (k & 1) * STEP;
-#pragma unroll
-                    for (int ks = 0; ks < D / 16; ++ks)
-                        tc_mma_ss(to, q_t + (ks >> 2) * 1024 + (ks & 3) * 2, k_t + (ks >> 2) * 512 + (ks & 3) * 2, QK, ks > 0);
-                    tc_commit(s_full + (k & 1) * 8);
-                    tc_commit(empty + slot * 8);
-                    if (alone) bar_arrive(empty + slot * 8);
-                    if (i + 1 == own) {                  // no products after these read q
-                        tc_commit(smem_at(&sh.q_empty));
-                        if (nt == 1 && mode == STEPS) bar_arrive(smem_at(&sh.q_empty));
+                constexpr uint32_t QK = product(Elem<T>::FORMAT, STEP, false), PV = product(Elem<T>::FORMAT, D, true);
+                const int s = warp - 8;
+                const uint32_t q_m = matrix(smem_at(q_s), 16), k_m = matrix(smem_at(kv_s), 16), v_m = matrix(smem_at(kv_s), 8192);
+                const uint32_t S_at = tmem + s * 128, O_at = tmem + 256 + s * 128;
+                const uint32_t full = smem_at(&sh.full[0]), empty = smem_at(&sh.empty[0]), s_full = smem_at(&sh.s_full[s][0]), p_full = smem_at(&sh.p_full[s][0]);
+                int kvn = 0, sn = 0;                         // loads before the group, steps of this stream so far
+                bool go = true;
+                for (int n = 0; go; ++n) {
+                    const int si = n % SEGS;
+                    if (!(go = bar_wait(smem_at(&sh.seg_full[si]), (n / SEGS) & 1, quit))) break;
+                    const int nt = sh.seg[si].t1 - sh.seg[si].t0;
+                    const Mode mode = mode_of(sh.seg[si].g);
+                    bar_arrive(smem_at(&sh.seg_empty[si]));
+                    if (nt <= 0) break;
+                    if (!(go = bar_wait(smem_at(&sh.q_full), n & 1, quit))) break;
+                    const uint32_t q_t = q_m + (mode == STEPS ? 0 : s) * (S::TILE >> 4);
+                    const int rounds = rounds_of(mode, nt), own = mode == STEPS ? (nt + 1 - s) / 2 : nt;         // this stream's steps
+                    const bool alone = mode != ROWS;         // a slot that this stream reads alone is given back for the other one too
+                    // scores of this stream's step i: number k of all, into buffer k & 1
+                    auto scores = [&](int i, int k) {
+                        const int at = kvn + key_place(mode, i, s), slot = at % NS;
+                        if (!bar_wait(full + slot * 8, (at / NS) & 1, quit)) return false;
+                        tc_after();
+                        const uint32_t k_t = k_m + slot * (S::SLOT >> 4), to = S_at + (k & 1) * STEP;
+    #pragma unroll
+                        for (int ks = 0; ks < D / 16; ++ks)
+                            tc_mma_ss(to, q_t + (ks >> 2) * 1024 + (ks & 3) * 2, k_t + (ks >> 2) * 512 + (ks & 3) * 2, QK, ks > 0);
+                        tc_commit(s_full + (k & 1) * 8);
+                        tc_commit(empty + slot * 8);
+                        if (alone) bar_arrive(empty + slot * 8);
+                        if (i + 1 == own) {                  // no products after these read q
+                            tc_commit(smem_at(&sh.q_empty));
+                            if (nt == 1 && mode == STEPS) bar_arrive(smem_at(&sh.q_empty));
+                        }
+                        return true;
+                    };
+                    // weights of step i, number k, times its values
+                    auto values = [&](int i, int k) {
+                        const int at = kvn + value_place(mode, rounds, i, s), slot = at % NS;
+                        if (!bar_wait(full + slot * 8, (at / NS) & 1, quit) || !bar_wait(p_full + (k & 1) * 8, (k >> 1) & 1, quit)) return false;
+                        tc_after();
+                        const uint32_t v_t = v_m + slot * (S::SLOT >> 4), from = S_at + (k & 1) * STEP;
+    #pragma unroll
+                        for (int ks = 0; ks < STEP / 16; ++ks) tc_mma_ts(O_at, from + ks * 8, v_t + ks * 128, PV, !(i == 0 && ks == 0));
+                        tc_commit(smem_at(&sh.pv[s]));
+                        tc_commit(empty + slot * 8);
+                        if (alone) bar_arrive(empty + slot * 8);
+                        if (i + 1 == own) tc_commit(smem_at(&sh.o_full[s]));
+                        return true;
+                    };
+                    auto skip = [&](int at) {                // an empty place
+                        if (!bar_wait(full + at % NS * 8, (at / NS) & 1, quit)) return false;
+                        bar_arrive(empty + at % NS * 8); bar_arrive(empty + at % NS * 8);
+                        return true;
+                    };
+                    for (int i = 0; i < min(rounds, 2); ++i) go = go && (i < own ? scores(i, sn + i) : skip(kvn + key_place(mode, i, s)));
+                    for (int i = 0; i < rounds && go; ++i) {
+                        go = i < own ? values(i, sn) : skip(kvn + value_place(mode, rounds, i, s));
+                        if (i + 2 < rounds) go = go && (i + 2 < own ? scores(i + 2, sn + 2) : skip(kvn + key_place(mode, i + 2, s)));
+                        sn += i < own;
                     }
-                    return true;
-                };
-                // weights of step i, number k, times its values
-                auto values = [&](int i, int k) {
-                    const int at = kvn + value_place(mode, rounds, i, s), slot = at % NS;
-                    if (!bar_wait(full + slot * 8, (at / NS) & 1, quit) || !bar_wait(p_full + (k & 1) * 8, (k >> 1) & 1, quit)) return false;
-                    tc_after();
-                    const uint32_t v_t = v_m + slot * (S::SLOT >> 4), from = S_at + (k & 1) * STEP;
-#pragma unroll
-                    for (int ks = 0; ks < STEP / 16; ++ks) tc_mma_ts(O_at, from + ks * 8, v_t + ks * 128, PV, !(i == 0 && ks == 0));
-                    tc_commit(smem_at(&sh.pv[s]));
-                    tc_commit(empty + slot * 8);
-                    if (alone) bar_arrive(empty + slot * 8);
-                    if (i + 1 == own) tc_commit(smem_at(&sh.o_full[s]));
-                    return true;
-                };
-                auto skip = [&](int at) {                // an empty place
-                    if (!bar_wait(full + at % NS * 8, (at / NS) & 1, quit)) return false;
-                    bar_arrive(empty + at % NS * 8); bar_arrive(empty + at % NS * 8);
-                    return true;
-                };
-                for (int i = 0; i < min(rounds, 2); ++i) go = go && (i < own ? scores(i, sn + i) : skip(kvn + key_place(mode, i, s)));
-                for (int i = 0; i < rounds && go; ++i) {
-                    go = i < own ? values(i, sn) : skip(kvn + value_place(mode, rounds, i, s));
-                    if (i + 2 < rounds) go = go && (i + 2 < own ? scores(i + 2, sn + 2) : skip(kvn + key_place(mode, i + 2, s)));
-                    sn += i < own;
+                    // the other stream has seen its loads of this group come
+                    bar_arrive(smem_at(&sh.group_done[s]));
+                    go = go && bar_wait(smem_at(&sh.group_done[1 - s]), n & 1, quit);
+                    kvn += loads_of(mode, nt);
                 }
-                // the other stream has seen its loads of this group come
-                bar_arrive(smem_at(&sh.group_done[s]));
-                go = go && bar_wait(smem_at(&sh.group_done[1 - s]), n & 1, quit);
-                kvn += loads_of(mode, nt);
-            }
-            if (!go) {                                   // what was issued ends before the tensor memory is given back
-                tc_commit(smem_at(&sh.drained[s]));
-                const long long since = clock64();
-                while (!bar_try(smem_at(&sh.drained[s]), 0) && clock64() - since < WAIT_CYCLES) { }
-            }
+                if (!go) {                                   // what was issued ends before the tensor memory is given back
+                    tc_commit(smem_at(&sh.drained[s]));
+                    const long long since = clock64();
+                    while (!bar_try(smem_at(&sh.drained[s]), 0) && clock64() - since < WAIT_CYCLES) { }
+                }
             }
             __syncwarp();
         } else if (warp == 10) {
@@ -1088,15 +1078,14 @@ constexpr int JOIN_THREADS = 256;
 template <int D, class T>
 __global__ void __launch_bounds__(JOIN_THREADS) hx_attend_join_kernel(const AttendArgs a) {
     hx_wait_for_primary();
-    __shared__ int64_t prefix[PLAN_ITEMS + 1], scan[JOIN_THREADS / 16];
-    __shared__ int count[PLAN_ITEMS];
+    __shared__ int64_t prefix[PLAN_ITEMS + 1], scan[JOIN_THREADS / 32];
     __shared__ uint4 anc[HX_TREE_MAX];
     __shared__ int link[HX_TREE_MAX];
     const int4 de = a.desc[blockIdx.x];
     const int tid = threadIdx.x;
     if (de.w) {
         Plan plan{};
-        if (a.planned) plan = make_plan(a, prefix, count, scan, gridDim.x, false);
+        if (a.planned) plan = make_plan(a, prefix, scan, gridDim.x, false);
         Walk w = begin_walk(a, plan, blockIdx.x, gridDim.x);
         Group g;
         int t0, t1;
@@ -1161,22 +1150,9 @@ bool encode(CUtensorMap* map, const char* base, int64_t width, int64_t rows, int
                      CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// A kernel between two launches of the one that takes all shared memory asks for the same split of it, once per device: the
-// multiprocessor would change it, and back, otherwise.
-template <class Kernel>
-cudaError_t same_carveout(Kernel kernel, bool* asked) {
-    int dev = 0;
-    cudaError_t e = cudaGetDevice(&dev);
-    if (e != cudaSuccess || asked[dev & 63]) return e;
-    e = cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
-    if (e == cudaSuccess) asked[dev & 63] = true;
-    return e;
-}
-
 template <int D, class T>
 cudaError_t launch(const HxCore& core, AttendArgs a, cudaStream_t s) {
     static size_t allowed[64];
-    static bool joined[64];
     Maps maps{};
     if (!encoder()) return cudaErrorNotSupported;
     const int64_t width = (int64_t)a.n_kv_heads * D, rows = (int64_t)(a.n_pages - 1) * a.page_rows + a.page_tokens;
@@ -1187,8 +1163,8 @@ cudaError_t launch(const HxCore& core, AttendArgs a, cudaStream_t s) {
     a.row_tiles = hx_ceil_div(a.max_q * a.group, GROUP_ROWS);
     const int64_t items = (int64_t)a.n * a.row_tiles;
     a.planned = items <= PLAN_ITEMS;
-    // Two heads to a block spare the joining of two streams (256 decoding sequences of 8 heads: 617 us against 720), alternate steps
-    // of one spread few groups further (4 sequences: 24 us against 33).
+    // Two heads to a block spare the joining of two streams (256 decoding sequences of 8 heads, 4,096 tokens at most: 650 us against
+    // 683), alternate steps of one spread few groups further (4 sequences: 30 us against 40; 32 trees of 21: 117 against 135).
     a.twin = items * (a.n_kv_heads / 2) >= core.n_sm;
     cudaError_t e = hx_opt_in_smem(hx_attend_kernel<D, T>, Shape<D>::SMEM, allowed, 0);
     if (e != cudaSuccess) return e;
@@ -1196,8 +1172,6 @@ cudaError_t launch(const HxCore& core, AttendArgs a, cudaStream_t s) {
     e = hx_launch_dependent(hx_attend_kernel<D, T>, dim3(blocks), dim3(THREADS), Shape<D>::SMEM, s, a, maps);
     if (e != cudaSuccess) return e;
     ++*core.launches;
-    e = same_carveout(hx_attend_join_kernel<D, T>, joined);
-    if (e != cudaSuccess) return e;
     e = hx_launch_dependent(hx_attend_join_kernel<D, T>, dim3(blocks), dim3(JOIN_THREADS), 0, s, a);
     if (e == cudaSuccess) ++*core.launches;
     return e;
