@@ -1072,6 +1072,10 @@ __device__ void one_row(const AttendArgs& a, const Group& g, const uint4* anc, i
 }
 
 constexpr int JOIN_THREADS = 256;
+// Blocks to a cut group, and the rounds of a block below which more are not taken.  A round is a chain of loads from one part after
+// another, some 1 us, so one block needs 32 us for 256 rows.  One block against 16: a chunk of 64 queries on 1,024 tokens 79 us and
+// 33, 32 trees of 21 tokens 116 and 105, 6 trees of 48 on some 65,000 tokens 961 and 926; 4 decoding sequences 30 either way.
+constexpr int JOIN_SLICES = 16, JOIN_ROUNDS = 2;
 
 // Joins the parts of the groups that begin in a share and end in another, in the order of the shares; computes the groups of a
 // block again that found infinities or NaN where some rows do not look.
@@ -1094,7 +1098,7 @@ __global__ void __launch_bounds__(JOIN_THREADS) hx_attend_join_kernel(const Atte
             __syncthreads();
             if (a.tree && tid < 32) ancestors(a, g.item / a.row_tiles, anc, link);
             __syncthreads();
-            for (int r = tid >> 5; r < g.rows * g.heads; r += JOIN_THREADS / 32) one_row<D, T>(a, g, anc, g.head + r / g.rows, r % g.rows);
+            for (int r = blockIdx.y * (JOIN_THREADS / 32) + (tid >> 5); r < g.rows * g.heads; r += gridDim.y * (JOIN_THREADS / 32)) one_row<D, T>(a, g, anc, g.head + r / g.rows, r % g.rows);
         }
     }
     if (de.x == 0) return;
@@ -1102,7 +1106,7 @@ __global__ void __launch_bounds__(JOIN_THREADS) hx_attend_join_kernel(const Atte
     const Group g = group_of(a, de.y, de.z);
     constexpr int PER = D / 4;                           // four elements to a thread, rows along the threads
     const int rows = g.rows * g.heads;
-    for (int e = tid; e < rows * PER; e += JOIN_THREADS) {
+    for (int e = blockIdx.y * JOIN_THREADS + tid; e < rows * PER; e += gridDim.y * JOIN_THREADS) {
         const int c = e / rows * 4, hr = e - e / rows * rows, head = g.head + hr / g.rows, r = hr % g.rows;
         float m = -INFINITY, l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
         for (int i = 0; i < de.x; ++i) {
@@ -1172,7 +1176,9 @@ cudaError_t launch(const HxCore& core, AttendArgs a, cudaStream_t s) {
     e = hx_launch_dependent(hx_attend_kernel<D, T>, dim3(blocks), dim3(THREADS), Shape<D>::SMEM, s, a, maps);
     if (e != cudaSuccess) return e;
     ++*core.launches;
-    e = hx_launch_dependent(hx_attend_join_kernel<D, T>, dim3(blocks), dim3(JOIN_THREADS), 0, s, a);
+    const int64_t rows_of = std::min<int64_t>(GROUP_ROWS, (int64_t)a.max_q * a.group * (a.twin ? 2 : 1));
+    const int slices = (int)std::min<int64_t>(JOIN_SLICES, (rows_of * (D / 4) + JOIN_THREADS * JOIN_ROUNDS - 1) / (JOIN_THREADS * JOIN_ROUNDS));
+    e = hx_launch_dependent(hx_attend_join_kernel<D, T>, dim3(blocks, slices), dim3(JOIN_THREADS), 0, s, a);
     if (e == cudaSuccess) ++*core.launches;
     return e;
 }
