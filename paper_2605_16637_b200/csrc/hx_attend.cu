@@ -698,7 +698,7 @@ __global__ void __launch_bounds__(THREADS, 1) hx_attend_kernel(const AttendArgs 
                         if (!bar_wait(full + slot * 8, (at / NS) & 1, quit)) return false;
                         tc_after();
                         const uint32_t k_t = k_m + slot * (S::SLOT >> 4), to = S_at + (k & 1) * STEP;
-    #pragma unroll
+#pragma unroll
                         for (int ks = 0; ks < D / 16; ++ks)
                             tc_mma_ss(to, q_t + (ks >> 2) * 1024 + (ks & 3) * 2, k_t + (ks >> 2) * 512 + (ks & 3) * 2, QK, ks > 0);
                         tc_commit(s_full + (k & 1) * 8);
@@ -716,7 +716,7 @@ __global__ void __launch_bounds__(THREADS, 1) hx_attend_kernel(const AttendArgs 
                         if (!bar_wait(full + slot * 8, (at / NS) & 1, quit) || !bar_wait(p_full + (k & 1) * 8, (k >> 1) & 1, quit)) return false;
                         tc_after();
                         const uint32_t v_t = v_m + slot * (S::SLOT >> 4), from = S_at + (k & 1) * STEP;
-    #pragma unroll
+#pragma unroll
                         for (int ks = 0; ks < STEP / 16; ++ks) tc_mma_ts(O_at, from + ks * 8, v_t + ks * 128, PV, !(i == 0 && ks == 0));
                         tc_commit(smem_at(&sh.pv[s]));
                         tc_commit(empty + slot * 8);
